@@ -285,6 +285,130 @@ q4nx_status q4nx_flowkv_decode_static(const uint16_t* d_q, const uint16_t* d_k, 
                                       void* d_o, q4nx_dtype o_dtype, hipStream_t stream);
 
 /*
+ * Between the projections and the attention of a layer: norm of queries and
+ * keys for each head, rotation, and the write into the KV cache.
+ *
+ * q4nx_kv_format: the cache that q4nx_kv_store writes.
+ *   Q4NX_KV_BF16  [B][G][L][d] bf16 each for K and V: for one sequence the
+ *                 cache that q4nx_flowkv_decode reads.
+ *   Q4NX_KV_Q4    4 bits a value, for q4nx_kv4_attention and q4nx_kv4_load:
+ *                 q4nx_kv4_cache_size bytes each for K and V.  The d values of
+ *                 a (sequence, group, position) are quantized in groups of 32
+ *                 by the rule of q4nx_quantize, and stand for
+ *                 RNE_bf16(RN_fp32(scale * code + offset)), as the weights do
+ *                 in q4nx_gemm.  Layout, with P = ceil(L/32)*32 positions and
+ *                 head = sequence * G + group: all codes, then all
+ *                 (scale, offset) bf16 pairs (4 bytes, scale first).
+ *                   K codes  [head][P][d/8][4]: byte b of word s holds value
+ *                            8s + b in bits 0-3 and 8s + 4 + b in bits 4-7
+ *                   K pairs  [head][P][d/32]
+ *                   V codes  [head][P/32][d/64][4 h][16 n][2 e][2 a][4 r]: the
+ *                            byte of position 32 blk + 16a + 4h + r holds value
+ *                            64 i + 32e + n in bits 0-3 and + 16 in bits 4-7
+ *                   V pairs  [head][P/32][d/32][4 h][2 a][4 r]
+ */
+typedef enum q4nx_kv_format {
+  Q4NX_KV_BF16 = 0,
+  Q4NX_KV_Q4 = 1,
+  Q4NX_KV_RANGE_MIN_ = -2147483647 - 1, /* see q4nx_status */
+  Q4NX_KV_RANGE_MAX_ = 2147483647
+} q4nx_kv_format;
+
+/* Bytes of one 4-bit cache (K or V) of B sequences, G groups, dimension d (64,
+ * 128 or 256) and L positions: B * G * ceil(L/32) * 32 * d * 5/8.  0 for
+ * arguments that the calls below refuse. */
+size_t q4nx_kv4_cache_size(int64_t B, int64_t G, int64_t d, int64_t L);
+
+typedef struct q4nx_kv_store_args {
+  const void* q;             /* device, in_dtype: token t's H x d queries start q_stride * t elements on */
+  const void* k;             /* device, in_dtype: its G x d keys, k_stride * t elements on */
+  const void* v;             /* device, in_dtype: its G x d values, v_stride * t elements on */
+  const int32_t* positions;  /* device, [T]: a token's position, for the rotation and in the cache */
+  const int32_t* seqs;       /* device, [T]: a token's sequence (0..B-1); NULL: all in sequence 0 */
+  const uint16_t* q_weight;  /* device, [d] bf16; NULL: queries are not normed */
+  const uint16_t* k_weight;  /* device, [d] bf16; NULL: keys are not normed */
+  const float* inv_freq;     /* device, [d/2] radians per position; NULL: no rotation */
+  uint16_t* q_out;           /* device, [T][H][d] bf16; may be q itself (bf16, q_stride = H d) */
+  void* k_cache;             /* device, the cache of `format` */
+  void* v_cache;
+  int64_t q_stride, k_stride, v_stride; /* at least H d, G d, G d, at most 2^32; multiples of 16 bytes */
+  int64_t T, H, G, d, B, L;  /* tokens, query heads, KV groups, head dimension, sequences, positions of the cache */
+  float weight_offset;       /* 1 for weights stored as w - 1 (Gemma), 0 for plain ones */
+  float eps;
+  q4nx_dtype in_dtype;
+  q4nx_kv_format format;
+} q4nx_kv_store_args;
+
+/*
+ * Device.  For each token t and head, with x the head's d values in float32:
+ *   y_i = x_i / sqrt(mean(x^2) + eps) * (weight_offset + w_i)   (q and k, where a weight is given)
+ *   a_i = positions[t] * inv_freq[i], i < d/2                   (taken in 64 bits)
+ *   o_i = y_i cos a_i - y_(i+d/2) sin a_i,  o_(i+d/2) = y_(i+d/2) cos a_i + y_i sin a_i   (q and k)
+ * and v unchanged; all in float32, rounded once: q to bf16 in q_out, k and v
+ * into row (seqs[t], group, positions[t]) of their caches.  The other rows of
+ * the caches keep their contents.  A token whose position lies outside 0..L-1
+ * or whose sequence lies outside 0..B-1 is padding: nothing of it is written,
+ * in q_out neither.  Two tokens of one call must not name the same row (the
+ * row's contents are not defined if they do).  d is 64, 128 or 256; H, G, B
+ * and B G lie in 1..65535, L in 1..2^30, T in 1..2^24.  Pointers are 16-byte
+ * aligned, positions and seqs 4-byte.
+ * Errors: Q4NX_ERR_INVALID_ARG (NULL pointer, unknown dtype or format,
+ * weight_offset not finite, eps not finite or negative), Q4NX_ERR_SHAPE,
+ * Q4NX_ERR_ALIGNMENT, Q4NX_ERR_HIP.
+ */
+q4nx_status q4nx_kv_store(const q4nx_kv_store_args* args, hipStream_t stream);
+
+/*
+ * Device.  The values that rows of a 4-bit cache stand for: K and V of
+ * (d_seqs[t], every group, d_positions[t]) to row t of d_k_out and d_v_out,
+ * [T][G][d] of out_dtype (exact in both types).  Rows of padding (as in
+ * q4nx_kv_store) are left as they were.  T * G is at most 2^32.
+ * Errors: Q4NX_ERR_INVALID_ARG, Q4NX_ERR_SHAPE, Q4NX_ERR_ALIGNMENT, Q4NX_ERR_HIP.
+ */
+q4nx_status q4nx_kv4_load(const void* d_k, const void* d_v, const int32_t* d_positions, const int32_t* d_seqs,
+                          int64_t T, int64_t G, int64_t d, int64_t B, int64_t L, void* d_k_out, void* d_v_out,
+                          q4nx_dtype out_dtype, hipStream_t stream);
+
+/* Bytes of the workspace q4nx_kv4_attention needs for a call with these
+ * arguments.  0 where it needs none, or if an argument is invalid. */
+size_t q4nx_kv4_workspace_size(int64_t B, int64_t T, int64_t H, int64_t G, int64_t d, int64_t L, int64_t window);
+
+/*
+ * Device.  Attention over a 4-bit cache: T query rows of each of B sequences,
+ * the last T positions of their sequence (T = 1: decode; T > 1: a chunk of a
+ * prompt, or drafted tokens, causal among themselves).  With n = d_lens[b]
+ * positions in sequence b (the T rows' own included, stored beforehand), row t
+ * stands at position p = n - T + t and
+ *   o[b][t][h] = sum_j softmax_j(scale * q[b][t][h] . k[b][g][j]) v[b][g][j],  g = h / (H/G),
+ *   j over 0..p (window == 0) or max(0, p-window+1)..p (window > 0).
+ * A row before the sequence's start (p < 0: an empty sequence, or one shorter
+ * than T) attends to nothing and is zero.
+ *   d_q    : device, [B][T][H][d] bf16
+ *   d_k,d_v: device, the 4-bit caches (Q4NX_KV_Q4) of B sequences, G groups,
+ *            L positions; only rows of the attended range are used
+ *   d_lens : device, [B] int32, 4-byte aligned; read as clamped to 0..L.  They
+ *            may change from replay to replay of a captured call.
+ *   H, G   : H a multiple of G, at most 16 G;  d: 64, 128 or 256
+ *   T      : 1..L, T H/G at most 2^20 - 16;  window: 0..2^30
+ *   d_o    : device, [B][T][H][d] of o_dtype; fully written
+ *   d_work : device, at least q4nx_kv4_workspace_size bytes, owned by the
+ *            caller (NULL where that is 0); contents on entry do not matter.
+ *            Calls that share a workspace must not overlap.
+ * Pointers are 16-byte aligned where nothing else is said.  Scores are float32
+ * sums of exact bf16 products, exponentials and sums float32; the weights of
+ * the values are rounded so finely that a float32 output keeps float32
+ * accuracy.  The order of the sums depends on B, T, H, G, d, L, window and the
+ * lengths alone: the same call gives the same bits every time.
+ * Errors: Q4NX_ERR_INVALID_ARG (NULL pointer, unknown dtype, non-finite
+ * scale), Q4NX_ERR_SHAPE, Q4NX_ERR_ALIGNMENT, Q4NX_ERR_BUFFER_TOO_SMALL,
+ * Q4NX_ERR_HIP.
+ */
+q4nx_status q4nx_kv4_attention(const uint16_t* d_q, const void* d_k, const void* d_v, const int32_t* d_lens,
+                               int64_t B, int64_t T, int64_t H, int64_t G, int64_t d, int64_t L, int64_t window,
+                               float scale, void* d_o, q4nx_dtype o_dtype, void* d_work, size_t work_bytes,
+                               hipStream_t stream);
+
+/*
  * The matrix product of q4nx_gemm, q4nx_mx_gemm and q4nx_gemm_bf16, with an
  * optional caller workspace (Sec. 3.1.2's tiled MM; the split along K is this
  * library's scheduling, not the paper's).

@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -32,11 +33,14 @@ Q4NX_MAX_BATCH = 8
 Q4NX_WEIGHTS_Q4NX = 0
 Q4NX_WEIGHTS_MXFP4 = 1
 Q4NX_WEIGHTS_BF16 = 2
+Q4NX_KV_BF16 = 0
+Q4NX_KV_Q4 = 1
 
 EXPORTED = ["q4nx_packed_size", "q4nx_pack", "q4nx_unpack", "q4nx_quantize", "q4nx_dequant", "q4nx_gemv",
             "q4nx_gemv_batched", "q4nx_gemm", "q4nx_gemm_bf16", "q4nx_flowkv_workspace_size",
             "q4nx_flowkv_decode", "q4nx_flowkv_decode_static", "q4nx_mx_packed_size", "q4nx_mx_pack", "q4nx_mx_unpack", "q4nx_mx_quantize", "q4nx_mx_dequant",
             "q4nx_mx_gemv", "q4nx_mx_gemv_batched", "q4nx_mx_gemm", "q4nx_gemm_workspace_size", "q4nx_gemm_ex", "q4nx_stream_read",
+            "q4nx_kv4_cache_size", "q4nx_kv_store", "q4nx_kv4_load", "q4nx_kv4_workspace_size", "q4nx_kv4_attention",
             "q4nx_status_str", "q4nx_last_error"]
 
 if not os.path.exists(LIB_PATH):
@@ -106,6 +110,17 @@ lib.q4nx_gemm_workspace_size.argtypes = [ctypes.c_int, _i64, _i64, _i64]
 lib.q4nx_gemm_workspace_size.restype = _sz
 lib.q4nx_gemm_ex.argtypes = [ctypes.c_int, _i64, _i64, _i64, _vp, _vp, _vp, ctypes.c_int, _vp, _sz, _vp]
 lib.q4nx_gemm_ex.restype = ctypes.c_int
+lib.q4nx_kv4_cache_size.argtypes = [_i64] * 4
+lib.q4nx_kv4_cache_size.restype = _sz
+lib.q4nx_kv_store.argtypes = [ctypes.c_char_p, _vp]  # the struct's bytes, packed by _KV_STORE_ARGS
+lib.q4nx_kv_store.restype = ctypes.c_int
+lib.q4nx_kv4_load.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _vp, _vp, ctypes.c_int, _vp]
+lib.q4nx_kv4_load.restype = ctypes.c_int
+lib.q4nx_kv4_workspace_size.argtypes = [_i64] * 7
+lib.q4nx_kv4_workspace_size.restype = _sz
+lib.q4nx_kv4_attention.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _i64, _i64, ctypes.c_float, _vp,
+                                   ctypes.c_int, _vp, _sz, _vp]
+lib.q4nx_kv4_attention.restype = ctypes.c_int
 lib.q4nx_stream_read.argtypes = [_vp, _sz, _vp, _vp]
 lib.q4nx_stream_read.restype = ctypes.c_int
 lib.q4nx_status_str.argtypes = [ctypes.c_int]
@@ -405,3 +420,106 @@ def q4nx_flowkv_decode_static(q, K, V, H: int, G: int, d: int, L: int, t: int, w
     _check(lib.q4nx_flowkv_decode_static(_dptr(q), _dptr(K), _dptr(V), H, G, d, L, t, window, scale, _dptr(o),
                                          _dtype_code(o), _stream(stream)),
            "q4nx_flowkv_decode_static")
+
+
+# q4nx_kv_store_args: 11 pointers, 9 int64, 2 floats, 2 enums.
+_KV_STORE_ARGS = struct.Struct("@11P9q2f2i")
+
+
+def q4nx_kv4_cache_size(B: int, G: int, d: int, L: int) -> int:
+    return int(lib.q4nx_kv4_cache_size(B, G, d, L))
+
+
+def _cache_bytes(B: int, G: int, d: int, L: int, kv_format: int) -> int:
+    """Bytes of one cache for its size check."""
+    return B * G * ((L + 31) >> 5) * 20 * d if kv_format == Q4NX_KV_Q4 else 2 * B * G * L * d
+
+
+def _rows(t, T: int, width: int, what: str):
+    """Pointer and row stride (elements) of T rows of `width` values: a contiguous tensor, or a view of whole rows
+    of a wider one, as a stacked projection's columns are."""
+    if not t.is_cuda:
+        raise ValueError("expected a GPU tensor")
+    if t.is_contiguous():
+        if t.numel() < T * width:
+            raise ValueError(f"{what}: {t.numel()} elements, need {T * width}")
+        return t.data_ptr(), width
+    if t.dim() != 2 or t.stride(1) != 1 or t.shape[0] < T or t.shape[1] < width:
+        raise ValueError(f"{what}: expected a contiguous tensor, or 2-d rows of at least {width} contiguous values")
+    return t.data_ptr(), t.stride(0)
+
+
+def _ints(t, n: int, what: str) -> int:
+    if t.dtype != _torch.int32:
+        raise ValueError(f"{what}: expected int32")
+    _need(t, 4 * n, what)
+    return _dptr(t)
+
+
+def q4nx_kv_store(q, k, v, positions, q_out, k_cache, v_cache, T: int, H: int, G: int, d: int, B: int, L: int,
+                  kv_format: int = Q4NX_KV_Q4, seqs=None, q_weight=None, k_weight=None, weight_offset: float = 1.0,
+                  eps: float = 1e-6, inv_freq=None, stream=None):
+    """Norm of the queries and keys of each head (where a weight[d] is given), rotation (where inv_freq[d/2] is given)
+    and cache write of T tokens: q[T][H*d], k and v [T][G*d] (float32 or bfloat16, rows of any stride) -> q_out[T][H][d]
+    bfloat16 and row (seqs[t], positions[t]) of the caches.  positions, seqs: int32 on the GPU; a token whose position
+    or sequence is out of range is padding."""
+    qp, qs = _rows(q, T, H * d, "q")
+    kp, ks = _rows(k, T, G * d, "k")
+    vp, vs = _rows(v, T, G * d, "v")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("q, k and v must share one dtype")
+    cache = _cache_bytes(B, G, d, L, kv_format)
+    _need(q_out, 2 * T * H * d, "q_out")
+    _need(k_cache, cache, "k_cache")
+    _need(v_cache, cache, "v_cache")
+    qw = kw = fr = sq = 0
+    if q_weight is not None:
+        _need(q_weight, 2 * d, "q_weight")
+        qw = _dptr(q_weight)
+    if k_weight is not None:
+        _need(k_weight, 2 * d, "k_weight")
+        kw = _dptr(k_weight)
+    if inv_freq is not None:
+        if inv_freq.dtype != _F32:
+            raise ValueError("inv_freq: expected float32")
+        _need(inv_freq, 2 * d, "inv_freq")
+        fr = _dptr(inv_freq)
+    if seqs is not None:
+        sq = _ints(seqs, T, "seqs")
+    args = _KV_STORE_ARGS.pack(qp, kp, vp, _ints(positions, T, "positions"), sq, qw, kw, fr, _dptr(q_out), _dptr(k_cache),
+                               _dptr(v_cache), qs, ks, vs, T, H, G, d, B, L, weight_offset, eps, _dtype_code(q), kv_format)
+    _check(lib.q4nx_kv_store(args, _stream(stream)), "q4nx_kv_store")
+
+
+def q4nx_kv4_load(k_cache, v_cache, positions, k_out, v_out, T: int, G: int, d: int, B: int, L: int, seqs=None,
+                  stream=None):
+    """k_out, v_out [T][G][d] (float32 or bfloat16) <- the values of rows (seqs[t], positions[t]) of 4-bit caches."""
+    cache = _cache_bytes(B, G, d, L, Q4NX_KV_Q4)
+    _need(k_cache, cache, "k_cache")
+    _need(v_cache, cache, "v_cache")
+    if v_out.dtype != k_out.dtype:
+        raise ValueError("k_out and v_out must share one dtype")
+    _need(k_out, T * G * d * k_out.element_size(), "k_out")
+    _need(v_out, T * G * d * v_out.element_size(), "v_out")
+    _check(lib.q4nx_kv4_load(_dptr(k_cache), _dptr(v_cache), _ints(positions, T, "positions"),
+                             None if seqs is None else _ints(seqs, T, "seqs"), T, G, d, B, L, _dptr(k_out), _dptr(v_out),
+                             _dtype_code(k_out), _stream(stream)), "q4nx_kv4_load")
+
+
+def q4nx_kv4_workspace_size(B: int, T: int, H: int, G: int, d: int, L: int, window: int = 0) -> int:
+    return int(lib.q4nx_kv4_workspace_size(B, T, H, G, d, L, window))
+
+
+def q4nx_kv4_attention(q, k_cache, v_cache, lens, B: int, T: int, H: int, G: int, d: int, L: int, window: int,
+                       scale: float, o, work=None, stream=None):
+    """o[B][T][H][d] <- attention of the queries q[B][T][H][d], the last T positions of sequences of lens[b] positions,
+    over 4-bit caches (window 0 = full attention)."""
+    cache = _cache_bytes(B, G, d, L, Q4NX_KV_Q4)
+    _need(q, 2 * B * T * H * d, "q")
+    _need(k_cache, cache, "k_cache")
+    _need(v_cache, cache, "v_cache")
+    _need(o, B * T * H * d * o.element_size(), "o")
+    wp, wn = (None, 0) if work is None else (_dptr(work), work.nbytes)
+    _check(lib.q4nx_kv4_attention(_dptr(q), _dptr(k_cache), _dptr(v_cache), _ints(lens, B, "lens"), B, T, H, G, d, L,
+                                  window, scale, _dptr(o), _dtype_code(o), wp, wn, _stream(stream)),
+           "q4nx_kv4_attention")

@@ -26,7 +26,7 @@ LIB = os.path.join(HERE, "libq4nx.so")
 ASAN_LIB = os.path.join(os.path.dirname(HERE), "_build", "libq4nx_asan.so")
 ARCH = "gfx950"
 
-SOURCES = ["q4nx_host.cpp", "q4nx_kernels.hip", "q4nx_flowkv.hip"]
+SOURCES = ["q4nx_host.cpp", "q4nx_kernels.hip", "q4nx_flowkv.hip", "q4nx_kv4.hip"]
 
 
 def hipcc() -> str:

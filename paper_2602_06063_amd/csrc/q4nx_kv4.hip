@@ -1,0 +1,842 @@
+// What lies between the q/k/v projections and the output projection of a
+// layer, for gfx950: the norm of queries and keys for each head, the rotation
+// and the cache write in one launch (q4nx_kv_store), the reader of cache rows
+// (q4nx_kv4_load), and attention over a cache held in 4 bits
+// (q4nx_kv4_attention).
+//
+// A 4-bit cache holds d values of a (sequence, KV group, position) in groups
+// of 32 with a bf16 scale and offset each, and stands for
+// RNE_bf16(RN_f32(scale * code + offset)), as the packed weights do in a
+// matrix product.  The two layouts are those that attention's matrix
+// instructions read without a transposition:
+//   K  operand rows are positions, so a position's codes lie together, 8
+//      values (one operand of a lane) to a 32-bit word: byte b holds values
+//      8s + b (low nibble) and 8s + 4 + b.
+//   V  operand rows are values and positions are what is summed over, so a
+//      block of 32 positions holds, for 64 values, [4 h][16 n][2 e][2 a][4 r]
+//      bytes: position 16a + 4h + r of values 32e + n (low nibble) and + 16.
+//      Lane 16h + n takes 16 bytes.  (16a + 4h + r is where the score product
+//      leaves position (a, r) in lane group h.)
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <string>
+#include <type_traits>
+
+#include "q4nx_device.h"
+#include "q4nx_eq3.h"
+#include "q4nx_internal.h"
+#include "q4nx_xlane.h"
+
+namespace q4nx {
+
+constexpr int kKvBlock = 32;  // positions of a V block; a cache's capacity is rounded up to whole blocks
+constexpr int64_t kMaxL = int64_t(1) << 30;
+
+static inline int64_t kv_positions(int64_t L) { return ceil_div(L, kKvBlock) * kKvBlock; }
+
+// ---------------------------------------------------------------------------
+// q4nx_kv_store
+// ---------------------------------------------------------------------------
+// D / 8 lanes take a row of one head: lane j holds values 4j..4j+3 and
+// D/2 + 4j..+3, so that both values of a rotated pair are in one lane and a
+// group of 32 values is 8 lanes.  A wave takes 64 / (D / 8) heads at a time
+// (queries, then keys, then values of one token), `passes` times.
+struct StoreArgs {
+  const void *q, *k, *v;
+  const int32_t *positions, *seqs;
+  const uint16_t *q_weight, *k_weight;
+  const float* inv_freq;
+  uint16_t* q_out;
+  uint8_t *k_cache, *v_cache;
+  int64_t q_stride, k_stride, v_stride;
+  int64_t P;         // positions of a head in the cache: L, or whole blocks
+  int64_t heads_P;   // B G P
+  int T, H, G, B, L;
+  int parts, passes; // waves of a token, and heads of a wave in steps of 64 / (D / 8)
+  float weight_offset, eps;
+};
+
+// 4 consecutive values of a row.
+template <bool F32>
+__device__ __forceinline__ f32x4 load4(const void* p, int64_t i) {
+  if constexpr (F32) {
+    return *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
+  } else {
+    const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+    return (f32x4){bf16_to_f32(v.x & 0xFFFFu), __uint_as_float(v.x & 0xFFFF0000u), bf16_to_f32(v.y & 0xFFFFu),
+                   __uint_as_float(v.y & 0xFFFF0000u)};
+  }
+}
+
+__device__ __forceinline__ uint2 bf16x4_bits(f32x4 v) {
+  return make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+}
+
+// Codes (a byte each) and the (scale, offset) word of a group of 32 values, 4
+// to a lane in 8 consecutive lanes: the conversion of q4nx_quantize.
+__device__ __forceinline__ uint32_t group_codes(f32x4 v, uint32_t& pair) {
+  float lo = INFINITY, hi = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[e] = v[e] != v[e] ? 0.0f : fminf(fmaxf(v[e], -kQuantClamp), kQuantClamp);
+    lo = fminf(lo, v[e]);
+    hi = fmaxf(hi, v[e]);
+  }
+  lo = fminf(lo, xor_lane<1>(lo));
+  hi = fmaxf(hi, xor_lane<1>(hi));
+  lo = fminf(lo, xor_lane<2>(lo));
+  hi = fmaxf(hi, xor_lane<2>(hi));
+  lo = fminf(lo, xor_lane<4>(lo)) + 0.0f;  // a zero minimum is +0
+  hi = fmaxf(hi, xor_lane<4>(hi));
+  const uint32_t sb = bf16_rne_flushed((hi - lo) / 15.0f), mb = bf16_rne_flushed(lo);
+  pair = sb | (mb << 16);
+  const float d = bf16_to_f32(sb), m = bf16_to_f32(mb);
+  const float inv = d == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(d);  // d = 0: every code is 0
+  const float R = fabsf(m) * inv, near = 0.5f - kQuantU * (128.0f + R);
+  uint32_t codes = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = (v[e] - m) * inv, c = rintf(x);
+    uint32_t q = (uint32_t)__builtin_amdgcn_fmed3f(c, 0.0f, 15.0f);
+    if (!(R <= kQuantMaxR && fabsf(x - c) <= near)) q = (uint32_t)quant_code(v[e], d, m);
+    codes |= q << (8 * e);
+  }
+  return codes;
+}
+
+template <int D, bool F32, bool Q4>
+__global__ __launch_bounds__(256) void kv_store_kernel(StoreArgs a) {
+  constexpr int R = D / 8, RW = 64 / R;
+  const int lane = threadIdx.x & 63, j = lane % R, sub = lane / R;
+  const int64_t wid = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t t = wid / a.parts;
+  if (t >= a.T) return;
+  const int part = (int)(wid - t * a.parts);
+  const int pos = a.positions[t];
+  const int seq = a.seqs ? a.seqs[t] : 0;
+  if (pos < 0 || pos >= a.L || seq < 0 || seq >= a.B) return;  // the whole wave: a padded token
+
+  const int e0 = part * a.passes * RW;
+  const int heads = a.H + 2 * a.G;
+  // The angle of pair i is pos * inv_freq[i], an exact product in 64 bits,
+  // whole turns taken off before it becomes float32: at position 10^5 a
+  // float32 angle is off by 2^-8 radians.  The turn's sine and cosine are
+  // good to some 2^-20, far below the 2^-9 of a stored value.
+  f32x4 cs = {1.0f, 1.0f, 1.0f, 1.0f}, sn = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (a.inv_freq && e0 < a.H + a.G) {
+    const f32x4 f = *reinterpret_cast<const f32x4*>(a.inv_freq + 4 * j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const double turns = (double)pos * (double)f[e] * 0.15915494309189535;
+      const float frac = (float)(turns - rint(turns));
+      sn[e] = __builtin_amdgcn_sinf(frac);
+      cs[e] = __builtin_amdgcn_cosf(frac);
+    }
+  }
+#pragma unroll 1
+  for (int s = 0; s < a.passes; ++s) {
+    const int h = e0 + s * RW + sub;
+    if (e0 + s * RW >= heads) break;
+    const bool is_q = h < a.H, is_k = !is_q && h < a.H + a.G, there = h < heads;
+    const int hk = is_q ? h : is_k ? h - a.H : there ? h - a.H - a.G : a.G - 1;
+    const void* src = is_q ? a.q : is_k ? a.k : a.v;
+    const int64_t at = t * (is_q ? a.q_stride : is_k ? a.k_stride : a.v_stride) + (int64_t)hk * D + 4 * j;
+    f32x4 x = load4<F32>(src, at), y = load4<F32>(src, at + D / 2);
+    const uint16_t* w = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
+    // Every lane takes part in the lane exchanges; values keep what they are.
+    float ss = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
+    ss += xor_lane<1>(ss);
+    ss += xor_lane<2>(ss);
+    ss += xor_lane<4>(ss);
+    if constexpr (R >= 16) ss += xor_lane<8>(ss);
+    if constexpr (R >= 32) ss += xor_lane<16>(ss);
+    if (w) {
+      const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+      const f32x4 wx = load4<false>(w, 4 * j), wy = load4<false>(w, D / 2 + 4 * j);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = x[e] * r * (a.weight_offset + wx[e]);
+        y[e] = y[e] * r * (a.weight_offset + wy[e]);
+      }
+    }
+    if (a.inv_freq && (is_q || is_k)) {  // (an infinite value times a sine of 0 would be NaN)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float lo = x[e] * cs[e] - y[e] * sn[e], hi = y[e] * cs[e] + x[e] * sn[e];
+        x[e] = lo;
+        y[e] = hi;
+      }
+    }
+    if (is_q) {
+      uint16_t* o = a.q_out + (t * a.H + h) * D + 4 * j;
+      *reinterpret_cast<uint2*>(o) = bf16x4_bits(x);
+      *reinterpret_cast<uint2*>(o + D / 2) = bf16x4_bits(y);
+    }
+    const int64_t head = (int64_t)seq * a.G + hk;
+    if constexpr (!Q4) {
+      if (there && !is_q) {
+        uint16_t* o = reinterpret_cast<uint16_t*>(is_k ? a.k_cache : a.v_cache) + (head * a.P + pos) * D + 4 * j;
+        *reinterpret_cast<uint2*>(o) = bf16x4_bits(x);
+        *reinterpret_cast<uint2*>(o + D / 2) = bf16x4_bits(y);
+      }
+    } else {
+      if (e0 + s * RW + RW <= a.H) continue;  // the whole wave: only queries
+      uint32_t pair[2], code[2] = {group_codes(x, pair[0]), group_codes(y, pair[1])};
+      const int u = j & 7, g0 = j >> 3;  // groups g0 and g0 + D / 64
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int g = g0 + i * (D / 64);
+        const uint32_t odd = (uint32_t)xor_lane_bits<1>((int)code[i]), far = (uint32_t)xor_lane_bits<4>((int)code[i]);
+        if (is_k) {
+          if ((u & 1) == 0)
+            *reinterpret_cast<uint32_t*>(a.k_cache + (head * a.P + pos) * (D / 2) + 16 * g + 2 * u) = code[i] | (odd << 4);
+          if (u == 0)
+            reinterpret_cast<uint32_t*>(a.k_cache + a.heads_P * (D / 2))[(head * a.P + pos) * (D / 32) + g] = pair[i];
+        } else if (there && !is_q) {
+          const int blk = pos >> 5, pa = (pos >> 4) & 1, ph = (pos >> 2) & 3, pr = pos & 3;
+          if (u < 4) {
+            const uint32_t both = code[i] | (far << 4);
+            uint8_t* o = a.v_cache + head * a.P * (D / 2) + (int64_t)blk * (16 * D) + (g >> 1) * 1024 +
+                         (ph * 16 + 4 * u) * 16 + (g & 1) * 8 + pa * 4 + pr;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) o[16 * b] = (uint8_t)(both >> (8 * b));
+          }
+          if (u == 0)
+            reinterpret_cast<uint32_t*>(a.v_cache + a.heads_P * (D / 2))[head * a.P * (D / 32) + (int64_t)blk * D +
+                                                                         g * 32 + ph * 8 + pa * 4 + pr] = pair[i];
+        }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// q4nx_kv4_load
+// ---------------------------------------------------------------------------
+// D / 8 lanes take a row: of K, lane j the word of values 8j..8j+7; of V, the
+// 4 bytes of values 32g + 4i..+3 and + 16 (g = j / 4, i = j % 4).
+template <int D, bool F32>
+__device__ __forceinline__ void store4(void* out, int64_t i, f32x4 v) {
+  if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + i) = v;
+  else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + i) = bf16x4_bits(v);
+}
+
+// Four codes (the bytes of `codes`) times the group's scale plus its offset,
+// rounded to bf16.
+__device__ __forceinline__ f32x4 values4(uint32_t codes, float d, float m) {
+  const uint32_t c = opaque(codes);
+  f32x4 v;
+  v[0] = fmaf((float)(c & 0xFFu), d, m);
+  v[1] = fmaf((float)((c >> 8) & 0xFFu), d, m);
+  v[2] = fmaf((float)((c >> 16) & 0xFFu), d, m);
+  v[3] = fmaf((float)(c >> 24), d, m);
+  const uint2 b = bf16x4_bits(v);
+  return (f32x4){bf16_to_f32(b.x & 0xFFFFu), __uint_as_float(b.x & 0xFFFF0000u), bf16_to_f32(b.y & 0xFFFFu),
+                 __uint_as_float(b.y & 0xFFFF0000u)};
+}
+
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void kv4_load_kernel(const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
+                                                       const int32_t* __restrict__ positions,
+                                                       const int32_t* __restrict__ seqs, void* __restrict__ k_out,
+                                                       void* __restrict__ v_out, int T, int G, int B, int L, int64_t P,
+                                                       int64_t heads_P) {
+  constexpr int R = D / 8;
+  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / R;
+  const int j = threadIdx.x % R;
+  if (row >= (int64_t)T * G) return;
+  const int64_t t = row / G;
+  const int g = (int)(row - t * G);
+  const int pos = positions[t], seq = seqs ? seqs[t] : 0;
+  if (pos < 0 || pos >= L || seq < 0 || seq >= B) return;
+  const int64_t head = (int64_t)seq * G + g;
+  {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(kc + (head * P + pos) * (D / 2) + 4 * j);
+    const uint32_t pr = reinterpret_cast<const uint32_t*>(kc + heads_P * (D / 2))[(head * P + pos) * (D / 32) + j / 4];
+    const float d = bf16_to_f32(pr & 0xFFFFu), m = __uint_as_float(pr & 0xFFFF0000u);
+    store4<D, F32>(k_out, row * D + 8 * j, values4(w & 0x0F0F0F0Fu, d, m));
+    store4<D, F32>(k_out, row * D + 8 * j + 4, values4((w >> 4) & 0x0F0F0F0Fu, d, m));
+  }
+  {
+    const int gr = j / 4, i = j % 4, blk = pos >> 5, pa = (pos >> 4) & 1, ph = (pos >> 2) & 3, pr4 = pos & 3;
+    const uint8_t* s = vc + head * P * (D / 2) + (int64_t)blk * (16 * D) + (gr >> 1) * 1024 + (ph * 16 + 4 * i) * 16 +
+                       (gr & 1) * 8 + pa * 4 + pr4;
+    const uint32_t w = s[0] | ((uint32_t)s[16] << 8) | ((uint32_t)s[32] << 16) | ((uint32_t)s[48] << 24);
+    const uint32_t pr = reinterpret_cast<const uint32_t*>(vc + heads_P * (D / 2))[head * P * (D / 32) + (int64_t)blk * D +
+                                                                                  gr * 32 + ph * 8 + pa * 4 + pr4];
+    const float d = bf16_to_f32(pr & 0xFFFFu), m = __uint_as_float(pr & 0xFFFF0000u);
+    store4<D, F32>(v_out, row * D + 32 * gr + 4 * i, values4(w & 0x0F0F0F0Fu, d, m));
+    store4<D, F32>(v_out, row * D + 32 * gr + 16 + 4 * i, values4((w >> 4) & 0x0F0F0F0Fu, d, m));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// q4nx_kv4_attention
+// ---------------------------------------------------------------------------
+struct AttnArgs {
+  const uint16_t* q;
+  const uint8_t *k, *v;
+  const int32_t* lens;
+  void* o;
+  float* work;
+  int64_t P, heads_P;
+  int T, H, G, L, window, rows;  // rows = T H / G of a KV group
+  int hg, splits;
+  float scale2;                  // scale * log2(e)
+};
+
+constexpr int kRowTile = 16, kAttnWaves = 4;
+
+// The blocks of 32 positions that a tile of rows attends to, and how many of
+// them a wave takes: shared by the two launches.
+struct TileRange {
+  int len, t0, t1, j0, j1;  // positions j0 .. j1 - 1 for rows t0 .. t1
+  int blk0, nblk, per;      // blocks, and blocks of a wave
+};
+__device__ __forceinline__ TileRange tile_range(const AttnArgs& a, int b, int tile) {
+  TileRange r;
+  r.len = min(max(a.lens[b], 0), a.L);
+  r.t0 = tile * kRowTile / a.hg;
+  r.t1 = min(a.T - 1, (tile * kRowTile + kRowTile - 1) / a.hg);
+  r.j1 = max(0, r.len - a.T + r.t1 + 1);
+  r.j0 = a.window ? max(0, max(0, r.len - a.T + r.t0) - a.window + 1) : 0;
+  r.blk0 = r.j0 / kKvBlock;
+  r.nblk = r.j1 > r.j0 ? (r.j1 + kKvBlock - 1) / kKvBlock - r.blk0 : 0;
+  const int nw = a.splits * kAttnWaves;
+  r.per = max(1, (r.nblk + nw - 1) / nw);
+  return r;
+}
+__device__ __forceinline__ int active_splits(const TileRange& r) {
+  return (r.nblk + r.per * kAttnWaves - 1) / (r.per * kAttnWaves);
+}
+
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// An output row's 4 values.
+__device__ __forceinline__ void put4(void* o, int bf16, int64_t i, f32x4 v) {
+  if (bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(o) + i) = bf16x4_bits(v);
+  else *reinterpret_cast<f32x4*>(static_cast<float*>(o) + i) = v;
+}
+
+// Eight codes of K (a word) as bf16 values in order.
+__device__ __forceinline__ u32x4 k_operand(uint32_t w, float d512, float m) {
+  const uint32_t lo = opaque(w & 0x0F0F0F0Fu), hi = opaque((w >> 4) & 0x0F0F0F0Fu);
+  const f32x2 a = codes2_f32<false>(lo), b = codes2_f32<true>(lo), c = codes2_f32<false>(hi), e = codes2_f32<true>(hi);
+  return (u32x4){pack_bf16x2(eq3(a[0], d512, m), eq3(a[1], d512, m)), pack_bf16x2(eq3(b[0], d512, m), eq3(b[1], d512, m)),
+                 pack_bf16x2(eq3(c[0], d512, m), eq3(c[1], d512, m)), pack_bf16x2(eq3(e[0], d512, m), eq3(e[1], d512, m))};
+}
+
+// Four codes (bytes) of V, each with the pair of its own position.
+__device__ __forceinline__ uint2 v_operand(uint32_t bytes, const float (&d)[4], const float (&m)[4]) {
+  const uint32_t c = opaque(bytes);
+  return make_uint2(pack_bf16x2(fmaf((float)(c & 0xFFu), d[0], m[0]), fmaf((float)((c >> 8) & 0xFFu), d[1], m[1])),
+                    pack_bf16x2(fmaf((float)((c >> 16) & 0xFFu), d[2], m[2]), fmaf((float)(c >> 24), d[3], m[3])));
+}
+
+// Scores and weighted values of 16 query rows of a KV group (T rows of H / G
+// heads, row = t H/G + h) over a part of the positions, on the matrix cores
+// as S^T = K Q^T and O^T = V^T P^T: a lane then holds the scores and the
+// outputs of one query row (lane % 16), so that a row's running maximum and
+// sum, and the correction of its outputs, are a lane's own, and the scores'
+// positions in lane group h are those of V's layout: nothing changes lanes
+// between the two products.
+//
+// grid (splits, row tiles, B G), 4 waves; each wave takes `per` blocks of 32
+// positions with a running maximum m and sum l (base 2), and the waves' states
+// are merged through LDS: into the output where the range is one workgroup's,
+// else into the workspace, for kv4_merge_kernel.
+//
+// The weights exp2(s - m) are rounded to bf16 for the product; NP of them, each
+// the rounding of what the ones before left, keep 8 NP bits: 3 for a float32
+// output, 2 for a bf16 one.
+template <int D, int NP>
+__global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
+  constexpr int NS = D / 32, NG = D / 32, NT = D / 16;  // K steps, V groups, output tiles
+  constexpr int kWords = D / 32;                        // words of K codes per lane and 16 positions
+  constexpr int kStride = D + 4;
+  __shared__ __attribute__((aligned(16))) float ys[kAttnWaves][kRowTile][kStride];
+  __shared__ float ms[kAttnWaves][kRowTile], ls[kAttnWaves][kRowTile];
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, h = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int split = blockIdx.x, tile = blockIdx.y, bg = blockIdx.z, b = bg / a.G, g = bg - b * a.G;
+  const TileRange r = tile_range(a, b, tile);
+  const int active = active_splits(r);
+  if (split >= max(active, 1)) return;  // the whole workgroup
+
+  const int row = tile * kRowTile + n;
+  const bool there = row < a.rows;
+  const int t = there ? row / a.hg : r.t1;
+  const int64_t q_row = ((int64_t)b * a.T + t) * a.H + g * a.hg + (there ? row - t * a.hg : 0);
+  const int pos = r.len - a.T + t;                                   // the row's own position
+  const int row_hi = pos, row_lo = a.window ? pos - a.window + 1 : 0;
+
+  // Q's operand: step s of lane group h covers the dims that K's words hold.
+  u32x4 qf[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const int dim = D == 64 ? 16 * h + 8 * s : (s / 4) * 128 + 32 * h + 8 * (s % 4);
+    qf[s] = there ? *reinterpret_cast<const u32x4*>(a.q + q_row * D + dim) : (u32x4){0, 0, 0, 0};
+  }
+
+  const uint8_t* kc = a.k + (int64_t)bg * a.P * (D / 2);
+  const uint32_t* kp = reinterpret_cast<const uint32_t*>(a.k + a.heads_P * (D / 2)) + (int64_t)bg * a.P * (D / 32);
+  const uint8_t* vc = a.v + (int64_t)bg * a.P * (D / 2);
+  const uint32_t* vp = reinterpret_cast<const uint32_t*>(a.v + a.heads_P * (D / 2)) + (int64_t)bg * a.P * (D / 32);
+
+  const int w0 = r.blk0 + (split * kAttnWaves + wave) * r.per;
+  const int w1 = min(r.blk0 + r.nblk, w0 + r.per);
+
+  uint32_t kw[2][kWords], kpair[2][D == 256 ? 2 : 1];
+  u32x4 vw[D / 64], vpair[NG][2];
+  const auto load_k = [&](int blk) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t p = (int64_t)blk * kKvBlock + 16 * i + n;
+      const uint8_t* c = kc + p * (D / 2);
+      if constexpr (D == 64) {
+        const uint2 w = *reinterpret_cast<const uint2*>(c + 8 * h);
+        kw[i][0] = w.x;
+        kw[i][1] = w.y;
+        kpair[i][0] = kp[p * 2 + (h >> 1)];
+      } else {
+#pragma unroll
+        for (int u = 0; u < D / 128; ++u) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(c + 64 * u + 16 * h);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) kw[i][4 * u + e] = w[e];
+          kpair[i][u] = kp[p * (D / 32) + 4 * u + h];
+        }
+      }
+    }
+  };
+  const auto load_v = [&](int blk) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < D / 64; ++u)
+      vw[u] = *reinterpret_cast<const u32x4*>(vc + (int64_t)blk * (16 * D) + u * 1024 + lane * 16);
+#pragma unroll
+    for (int u = 0; u < NG; ++u)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        vpair[u][i] = *reinterpret_cast<const u32x4*>(vp + (int64_t)blk * D + u * 32 + h * 8 + i * 4);
+  };
+
+  float m = -INFINITY, l = 0.0f;
+  f32x4 y[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) y[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+  if (w0 < w1) {
+    load_k(w0);
+    load_v(w0);
+  }
+#pragma unroll 1
+  for (int blk = w0; blk < w1; ++blk) {
+    const int p0 = blk * kKvBlock;
+    f32x4 s[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      s[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int u = 0; u < NS; ++u) {
+        const uint32_t pr = kpair[i][D == 256 ? u / 4 : 0];
+        s[i] = mfma16(k_operand(kw[i][u], bf16_to_f32(pr & 0xFFFFu) * 512.0f, __uint_as_float(pr & 0xFFFF0000u)), qf[u], s[i]);
+      }
+    }
+    if (blk + 1 < w1) load_k(blk + 1);
+    // Running maximum, weights, correction.
+    float mx = m;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int p = p0 + 16 * i + 4 * h + e;
+        s[i][e] = p <= row_hi && p >= row_lo ? s[i][e] * a.scale2 : -INFINITY;
+        mx = fmaxf(mx, s[i][e]);
+      }
+    mx = fmaxf(mx, xor_lane<16>(mx));
+    mx = fmaxf(mx, xor_lane<32>(mx));
+    const float base = mx == -INFINITY ? 0.0f : mx;  // nothing seen yet: every weight is exp2(-inf) = 0
+    const float corr = __builtin_amdgcn_exp2f(m - base);
+    m = mx;
+    l *= corr;
+    u32x4 pf[NP];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float f[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[e] = __builtin_amdgcn_exp2f(s[i][e] - base);
+        l += f[e];
+      }
+#pragma unroll
+      for (int k = 0; k < NP; ++k) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t w = pack_bf16x2(f[2 * e], f[2 * e + 1]);
+          pf[k][2 * i + e] = w;
+          f[2 * e] -= bf16_to_f32(w & 0xFFFFu);
+          f[2 * e + 1] -= __uint_as_float(w & 0xFFFF0000u);
+        }
+      }
+    }
+    // Rows of the block that no query row attends to hold anything: a pair of
+    // zeros makes them 0, whatever their codes.
+    if (p0 < r.j0 || p0 + kKvBlock > r.j1) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int p = p0 + 16 * i + 4 * h + e;
+          if (p < r.j0 || p >= r.j1) {
+#pragma unroll
+            for (int u = 0; u < NG; ++u) vpair[u][i][e] = 0;
+          }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) y[i] *= corr;
+#pragma unroll
+    for (int u = 0; u < NG; ++u) {
+      u32x4 lo, hi;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float d[4], mm[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          d[e] = bf16_to_f32(vpair[u][i][e] & 0xFFFFu);
+          mm[e] = __uint_as_float(vpair[u][i][e] & 0xFFFF0000u);
+        }
+        const uint32_t w = vw[u / 2][2 * (u & 1) + i];
+        const uint2 x = v_operand(w & 0x0F0F0F0Fu, d, mm), z = v_operand((w >> 4) & 0x0F0F0F0Fu, d, mm);
+        lo[2 * i] = x.x;
+        lo[2 * i + 1] = x.y;
+        hi[2 * i] = z.x;
+        hi[2 * i + 1] = z.y;
+      }
+#pragma unroll
+      for (int k = 0; k < NP; ++k) {
+        y[2 * u] = mfma16(lo, pf[k], y[2 * u]);
+        y[2 * u + 1] = mfma16(hi, pf[k], y[2 * u + 1]);
+      }
+    }
+    if (blk + 1 < w1) load_v(blk + 1);
+  }
+  l += xor_lane<16>(l);
+  l += xor_lane<32>(l);
+
+  if (there) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) *reinterpret_cast<f32x4*>(&ys[wave][n][16 * i + 4 * h]) = y[i];
+    if (h == 0) {
+      ms[wave][n] = m;
+      ls[wave][n] = l;
+    }
+  }
+  __syncthreads();
+  const int nrows = min(kRowTile, a.rows - tile * kRowTile);
+  for (int e = tid; e < nrows * (D / 4); e += 64 * kAttnWaves) {
+    const int rr = e / (D / 4), dd = 4 * (e - rr * (D / 4));
+    float mx = ms[0][rr];
+#pragma unroll
+    for (int w = 1; w < kAttnWaves; ++w) mx = fmaxf(mx, ms[w][rr]);
+    const float base = mx == -INFINITY ? 0.0f : mx;
+    float lt = 0.0f;
+    f32x4 yt = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w) {
+      const float c = __builtin_amdgcn_exp2f(ms[w][rr] - base);
+      lt = fmaf(c, ls[w][rr], lt);
+      yt += c * *reinterpret_cast<const f32x4*>(&ys[w][rr][dd]);
+    }
+    if (active <= 1) {
+      const int R = tile * kRowTile + rr, tt = R / a.hg;
+      const int64_t o = (((int64_t)b * a.T + tt) * a.H + g * a.hg + R - tt * a.hg) * D + dd;
+      // A row that attends to nothing is zero.
+      put4(a.o, NP == 2, o, lt == 0.0f ? (f32x4){0.0f, 0.0f, 0.0f, 0.0f} : yt / lt);
+    } else {
+      float* part = a.work + ((((int64_t)bg * gridDim.y + tile) * a.splits + split) * kRowTile + rr) * (D + 4);
+      *reinterpret_cast<f32x4*>(part + 4 + dd) = yt;
+      if (dd == 0) {
+        part[0] = mx;
+        part[1] = lt;
+      }
+    }
+  }
+}
+
+// Merges the splits of a row: grid (rows, row tiles -> flattened, D / 64) ...
+// workgroup (row of a group, B G, 64 values), 4 waves that take the splits in
+// turn; the sums run over a wave's splits in increasing order and then over
+// the waves.
+template <int D>
+__global__ __launch_bounds__(256) void kv4_merge_kernel(AttnArgs a, int tiles, int bf16) {
+  __shared__ float ys[4][64], ls[4], ms[4];
+  const int row = blockIdx.x, bg = blockIdx.y, b = bg / a.G, g = bg - b * a.G;
+  const int tile = row / kRowTile;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, dim = blockIdx.z * 64 + lane;
+  const TileRange r = tile_range(a, b, tile);
+  const int active = active_splits(r);
+  if (active <= 1) return;  // the first launch has written it
+  const float* part = a.work + (((int64_t)bg * tiles + tile) * a.splits * kRowTile + row % kRowTile) * (D + 4);
+  const int64_t step = (int64_t)kRowTile * (D + 4);
+  float m = -INFINITY;
+  for (int s = threadIdx.x; s < active; s += 256) m = fmaxf(m, part[s * step]);
+  m = fmaxf(m, xor_lane<1>(m));
+  m = fmaxf(m, xor_lane<2>(m));
+  m = fmaxf(m, xor_lane<4>(m));
+  m = fmaxf(m, xor_lane<8>(m));
+  m = fmaxf(m, xor_lane<16>(m));
+  m = fmaxf(m, xor_lane<32>(m));
+  if (lane == 0) ms[wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
+  const float base = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f, y = 0.0f;
+#pragma unroll 4
+  for (int s = wave; s < active; s += 4) {
+    const float c = __builtin_amdgcn_exp2f(part[s * step] - base);
+    l = fmaf(c, part[s * step + 1], l);
+    y = fmaf(c, part[s * step + 4 + dim], y);
+  }
+  ys[wave][lane] = y;
+  if (lane == 0) ls[wave] = l;
+  __syncthreads();
+  if (wave == 0) {
+    const float lt = ls[0] + ls[1] + ls[2] + ls[3];
+    const float yt = ys[0][lane] + ys[1][lane] + ys[2][lane] + ys[3][lane];
+    const float o = lt == 0.0f ? 0.0f : yt / lt;
+    const int t = row / a.hg;
+    const int64_t i = (((int64_t)b * a.T + t) * a.H + g * a.hg + row - t * a.hg) * D + dim;
+    if (bf16) static_cast<uint16_t*>(a.o)[i] = f32_to_bf16_bits(o);
+    else static_cast<float*>(a.o)[i] = o;
+  }
+}
+
+// Workgroups of the first launch: about two per CU, none with less than a
+// block of positions for each wave at the longest range that the call allows
+// (lengths are known on the device only).
+constexpr int kAttnGroups = 512;
+struct AttnPlan {
+  int64_t rows, tiles;
+  int splits;
+};
+static AttnPlan attn_plan(int64_t B, int64_t T, int64_t H, int64_t G, int64_t L, int64_t window) {
+  AttnPlan p;
+  p.rows = T * (H / G);
+  p.tiles = ceil_div(p.rows, kRowTile);
+  const int64_t span = window ? std::min(L, window + std::min<int64_t>(T, kRowTile)) : L;
+  const int64_t blocks = ceil_div(span, kKvBlock) + 1;
+  p.splits = (int)std::max<int64_t>(1, std::min(kAttnGroups / (B * G * p.tiles), ceil_div(blocks, kAttnWaves)));
+  return p;
+}
+static size_t attn_work_bytes(const AttnPlan& p, int64_t BG, int64_t d) {
+  return p.splits == 1 ? 0 : (size_t)(BG * p.tiles * p.splits * kRowTile * (d + 4)) * sizeof(float);
+}
+
+template <int D>
+static void launch_attention(const AttnArgs& a, const AttnPlan& p, int64_t BG, bool bf16, hipStream_t stream) {
+  const dim3 grid(p.splits, (unsigned)p.tiles, (unsigned)BG);
+  if (bf16) hipLaunchKernelGGL((kv4_rows_kernel<D, 2>), grid, dim3(64 * kAttnWaves), 0, stream, a);
+  else hipLaunchKernelGGL((kv4_rows_kernel<D, 3>), grid, dim3(64 * kAttnWaves), 0, stream, a);
+  if (p.splits > 1)
+    hipLaunchKernelGGL((kv4_merge_kernel<D>), dim3((unsigned)p.rows, (unsigned)BG, D / 64), dim3(256), 0, stream, a,
+                       (int)p.tiles, (int)bf16);
+}
+
+// ---- launchers ------------------------------------------------------------
+template <int D, bool F32, bool Q4>
+static void launch_store(const StoreArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((kv_store_kernel<D, F32, Q4>), dim3((unsigned)ceil_div((int64_t)a.T * a.parts, 4)), dim3(256), 0,
+                     stream, a);
+}
+
+template <int D>
+static void dispatch_store(StoreArgs a, bool f32, bool q4, hipStream_t stream) {
+  constexpr int RW = 512 / D;
+  const int64_t steps = ceil_div(a.H + 2 * (int64_t)a.G, RW);
+  // A wave per head group while there are few of them, and whole tokens (the
+  // angles taken once) where there are many.
+  a.passes = (int)std::max<int64_t>(1, std::min(steps, a.T * steps / 8192));
+  a.parts = (int)ceil_div(steps, a.passes);
+  if (f32 && q4) launch_store<D, true, true>(a, stream);
+  else if (f32) launch_store<D, true, false>(a, stream);
+  else if (q4) launch_store<D, false, true>(a, stream);
+  else launch_store<D, false, false>(a, stream);
+}
+
+static q4nx_status launched(const char* fn) {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(Q4NX_ERR_HIP, std::string(fn) + ": " + hipGetErrorString(e));
+  return Q4NX_OK;
+}
+
+// The checks that the three calls share: heads, head dimension and the cache.
+static q4nx_status check_cache(int64_t H, int64_t G, int64_t d, int64_t B, int64_t L, int64_t T, const char* fn) {
+  const std::string f(fn);
+  if (d != 64 && d != 128 && d != 256) return fail(Q4NX_ERR_SHAPE, f + ": d must be 64, 128 or 256");
+  if (H <= 0 || G <= 0 || B <= 0 || H > 65535 || G > 65535 || B > 65535 || B * G > 65535)
+    return fail(Q4NX_ERR_SHAPE, f + ": H, G, B and B G must lie in 1..65535");
+  if (L <= 0 || L > kMaxL) return fail(Q4NX_ERR_SHAPE, f + ": L must lie in 1..2^30");
+  if (T <= 0 || T > (int64_t(1) << 24)) return fail(Q4NX_ERR_SHAPE, f + ": T must lie in 1..2^24");
+  return Q4NX_OK;
+}
+
+}  // namespace q4nx
+
+using namespace q4nx;
+
+extern "C" {
+
+size_t q4nx_kv4_cache_size(int64_t B, int64_t G, int64_t d, int64_t L) {
+  if ((d != 64 && d != 128 && d != 256) || B <= 0 || G <= 0 || B > 65535 || G > 65535 || B * G > 65535 || L <= 0 || L > kMaxL)
+    return 0;
+  return (size_t)(B * G) * (size_t)kv_positions(L) * (size_t)(d / 32) * 20;
+}
+
+q4nx_status q4nx_kv_store(const q4nx_kv_store_args* args, hipStream_t stream) {
+  clear_error();
+  const std::string f("q4nx_kv_store");
+  if (!args) return fail(Q4NX_ERR_INVALID_ARG, f + ": NULL pointer");
+  const q4nx_kv_store_args& s = *args;
+  if (!s.q || !s.k || !s.v || !s.positions || !s.q_out || !s.k_cache || !s.v_cache)
+    return fail(Q4NX_ERR_INVALID_ARG, f + ": NULL pointer");
+  if (s.in_dtype != Q4NX_F32 && s.in_dtype != Q4NX_BF16) return fail(Q4NX_ERR_INVALID_ARG, f + ": unknown in_dtype");
+  if (s.format != Q4NX_KV_BF16 && s.format != Q4NX_KV_Q4) return fail(Q4NX_ERR_INVALID_ARG, f + ": unknown cache format");
+  if (!std::isfinite(s.weight_offset) || !std::isfinite(s.eps) || s.eps < 0.0f)
+    return fail(Q4NX_ERR_INVALID_ARG, f + ": weight_offset must be finite, eps finite and not negative");
+  if (q4nx_status st = check_cache(s.H, s.G, s.d, s.B, s.L, s.T, f.c_str())) return st;
+  const int64_t stride_max = int64_t(1) << 32;
+  if (s.q_stride < s.H * s.d || s.k_stride < s.G * s.d || s.v_stride < s.G * s.d || s.q_stride > stride_max ||
+      s.k_stride > stride_max || s.v_stride > stride_max)
+    return fail(Q4NX_ERR_SHAPE, f + ": a row stride is shorter than its row, or above 2^32");
+  const bool f32 = s.in_dtype == Q4NX_F32, q4 = s.format == Q4NX_KV_Q4;
+  const int per16 = f32 ? 4 : 8;
+  if (!aligned(s.q, 16) || !aligned(s.k, 16) || !aligned(s.v, 16) || s.q_stride % per16 || s.k_stride % per16 ||
+      s.v_stride % per16)
+    return fail(Q4NX_ERR_ALIGNMENT, f + ": the rows of q, k and v need 16-byte alignment");
+  if (!aligned(s.q_weight, 16) || !aligned(s.k_weight, 16) || !aligned(s.inv_freq, 16) || !aligned(s.q_out, 16) ||
+      !aligned(s.k_cache, 16) || !aligned(s.v_cache, 16) || !aligned(s.positions, 4) || !aligned(s.seqs, 4))
+    return fail(Q4NX_ERR_ALIGNMENT, f + ": weights, inv_freq, q_out and caches need 16-byte alignment, positions and seqs 4-byte");
+  StoreArgs a;
+  a.q = s.q;
+  a.k = s.k;
+  a.v = s.v;
+  a.positions = s.positions;
+  a.seqs = s.seqs;
+  a.q_weight = s.q_weight;
+  a.k_weight = s.k_weight;
+  a.inv_freq = s.inv_freq;
+  a.q_out = s.q_out;
+  a.k_cache = static_cast<uint8_t*>(s.k_cache);
+  a.v_cache = static_cast<uint8_t*>(s.v_cache);
+  a.q_stride = s.q_stride;
+  a.k_stride = s.k_stride;
+  a.v_stride = s.v_stride;
+  a.P = q4 ? kv_positions(s.L) : s.L;
+  a.heads_P = s.B * s.G * a.P;
+  a.T = (int)s.T;
+  a.H = (int)s.H;
+  a.G = (int)s.G;
+  a.B = (int)s.B;
+  a.L = (int)s.L;
+  a.weight_offset = s.weight_offset;
+  a.eps = s.eps;
+  if (s.d == 64) dispatch_store<64>(a, f32, q4, stream);
+  else if (s.d == 128) dispatch_store<128>(a, f32, q4, stream);
+  else dispatch_store<256>(a, f32, q4, stream);
+  return launched("q4nx_kv_store");
+}
+
+q4nx_status q4nx_kv4_load(const void* d_k, const void* d_v, const int32_t* d_positions, const int32_t* d_seqs, int64_t T,
+                          int64_t G, int64_t d, int64_t B, int64_t L, void* d_k_out, void* d_v_out, q4nx_dtype out_dtype,
+                          hipStream_t stream) {
+  clear_error();
+  const std::string f("q4nx_kv4_load");
+  if (!d_k || !d_v || !d_positions || !d_k_out || !d_v_out) return fail(Q4NX_ERR_INVALID_ARG, f + ": NULL pointer");
+  if (out_dtype != Q4NX_F32 && out_dtype != Q4NX_BF16) return fail(Q4NX_ERR_INVALID_ARG, f + ": unknown out_dtype");
+  if (q4nx_status st = check_cache(G, G, d, B, L, T, f.c_str())) return st;
+  if (!aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_k_out, 16) || !aligned(d_v_out, 16) ||
+      !aligned(d_positions, 4) || !aligned(d_seqs, 4))
+    return fail(Q4NX_ERR_ALIGNMENT, f + ": caches and outputs need 16-byte alignment, positions and seqs 4-byte");
+  if (T * G > (int64_t(1) << 32)) return fail(Q4NX_ERR_SHAPE, f + ": T G must not exceed 2^32");
+  const int64_t P = kv_positions(L);
+  const dim3 grid((unsigned)ceil_div(T * G * (d / 8), 256));
+  const auto go = [&](auto dc, auto fc) {
+    hipLaunchKernelGGL((kv4_load_kernel<decltype(dc)::value, decltype(fc)::value>), grid, dim3(256), 0, stream,
+                       static_cast<const uint8_t*>(d_k), static_cast<const uint8_t*>(d_v), d_positions, d_seqs, d_k_out,
+                       d_v_out, (int)T, (int)G, (int)B, (int)L, P, B * G * P);
+  };
+  const auto type = [&](auto dc) {
+    if (out_dtype == Q4NX_F32) go(dc, std::true_type{});
+    else go(dc, std::false_type{});
+  };
+  if (d == 64) type(std::integral_constant<int, 64>{});
+  else if (d == 128) type(std::integral_constant<int, 128>{});
+  else type(std::integral_constant<int, 256>{});
+  return launched("q4nx_kv4_load");
+}
+
+// Shapes that q4nx_kv4_attention and its workspace size accept.
+static q4nx_status check_attention(int64_t B, int64_t T, int64_t H, int64_t G, int64_t d, int64_t L, int64_t window) {
+  const std::string f("q4nx_kv4_attention");
+  if (q4nx_status st = check_cache(H, G, d, B, L, T, f.c_str())) return st;
+  if (H % G != 0 || H / G > 16) return fail(Q4NX_ERR_SHAPE, f + ": H must be a multiple of G, at most 16 of it");
+  if (T > L) return fail(Q4NX_ERR_SHAPE, f + ": T must not exceed L");
+  if (T * (H / G) > 65535 * (int64_t)kRowTile) return fail(Q4NX_ERR_SHAPE, f + ": T H / G must not exceed 2^20 - 16");
+  if (window < 0 || window > kMaxL) return fail(Q4NX_ERR_SHAPE, f + ": window must lie in 0..2^30");
+  return Q4NX_OK;
+}
+
+size_t q4nx_kv4_workspace_size(int64_t B, int64_t T, int64_t H, int64_t G, int64_t d, int64_t L, int64_t window) {
+  clear_error();
+  if (check_attention(B, T, H, G, d, L, window)) return 0;
+  return attn_work_bytes(attn_plan(B, T, H, G, L, window), B * G, d);
+}
+
+q4nx_status q4nx_kv4_attention(const uint16_t* d_q, const void* d_k, const void* d_v, const int32_t* d_lens, int64_t B,
+                               int64_t T, int64_t H, int64_t G, int64_t d, int64_t L, int64_t window, float scale,
+                               void* d_o, q4nx_dtype o_dtype, void* d_work, size_t work_bytes, hipStream_t stream) {
+  clear_error();
+  const std::string f("q4nx_kv4_attention");
+  if (!d_q || !d_k || !d_v || !d_lens || !d_o) return fail(Q4NX_ERR_INVALID_ARG, f + ": NULL pointer");
+  if (o_dtype != Q4NX_F32 && o_dtype != Q4NX_BF16) return fail(Q4NX_ERR_INVALID_ARG, f + ": unknown o_dtype");
+  if (!std::isfinite(scale)) return fail(Q4NX_ERR_INVALID_ARG, f + ": scale must be finite");
+  if (q4nx_status st = check_attention(B, T, H, G, d, L, window)) return st;
+  if (!aligned(d_q, 16) || !aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_o, 16) || !aligned(d_work, 16) ||
+      !aligned(d_lens, 4))
+    return fail(Q4NX_ERR_ALIGNMENT, f + ": q, caches, o and the workspace need 16-byte alignment, lens 4-byte");
+  const AttnPlan p = attn_plan(B, T, H, G, L, window);
+  const size_t need = attn_work_bytes(p, B * G, d);
+  if (need && !d_work) return fail(Q4NX_ERR_INVALID_ARG, f + ": NULL workspace");
+  if (work_bytes < need) return fail(Q4NX_ERR_BUFFER_TOO_SMALL, f + ": workspace smaller than q4nx_kv4_workspace_size");
+  AttnArgs a;
+  a.q = d_q;
+  a.k = static_cast<const uint8_t*>(d_k);
+  a.v = static_cast<const uint8_t*>(d_v);
+  a.lens = d_lens;
+  a.o = d_o;
+  a.work = static_cast<float*>(d_work);
+  a.P = kv_positions(L);
+  a.heads_P = B * G * a.P;
+  a.T = (int)T;
+  a.H = (int)H;
+  a.G = (int)G;
+  a.L = (int)L;
+  a.window = (int)window;
+  a.rows = (int)p.rows;
+  a.hg = (int)(H / G);
+  a.splits = p.splits;
+  a.scale2 = scale * 1.4426950408889634f;
+  const bool bf16 = o_dtype == Q4NX_BF16;
+  if (d == 64) launch_attention<64>(a, p, B * G, bf16, stream);
+  else if (d == 128) launch_attention<128>(a, p, B * G, bf16, stream);
+  else launch_attention<256>(a, p, B * G, bf16, stream);
+  return launched("q4nx_kv4_attention");
+}
+
+}  // extern "C"
