@@ -617,17 +617,292 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(AttnArgs a, int tiles, i
   }
 }
 
-// Workgroups of the first launch: about two per CU, none with less than a
-// block of positions for each wave at the longest range that the call allows
-// (lengths are known on the device only).
+// ---- many rows --------------------------------------------------------------
+// With many query rows of a group every tile of them needs the same values of
+// K and V, so these are expanded once, to bf16 in the workspace, in the order
+// in which the matrix instructions take them: the attention kernel then copies
+// whole kilobytes and dequantizes nothing.
+//   K  [B G][block][D/16 c][2 h][32 p][8 e]: value 16c + 8h + e of position p
+//   V  [B G][block][D/32 i][2 s][2 h][32 m][8 e]: value 32i + m of position
+//      16s + 8 (e / 4) + 4h + e % 4, where the score product of 32 positions
+//      leaves the weights of lane half h
+// Positions that no row attends to are zeros.
+constexpr int kExpandGroups = 2048;
+
+// The first block that any row of the sequence attends to.
+__device__ __forceinline__ int first_block(const AttnArgs& a, int len) {
+  return a.window ? max(0, max(0, len - a.T) - a.window + 1) / kKvBlock : 0;
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void kv4_expand_kernel(AttnArgs a, u32x4* __restrict__ ko, u32x4* __restrict__ vo,
+                                                         int cap) {
+  const int bg = blockIdx.y, b = bg / a.G;
+  const int len = min(max(a.lens[b], 0), a.L);
+  const int base = first_block(a, len), nblk = (len + kKvBlock - 1) / kKvBlock - base;
+  const int j0 = a.window ? max(0, max(0, len - a.T) - a.window + 1) : 0;
+  const uint8_t* kc = a.k + (int64_t)bg * a.P * (D / 2);
+  const uint32_t* kp = reinterpret_cast<const uint32_t*>(a.k + a.heads_P * (D / 2)) + (int64_t)bg * a.P * (D / 32);
+  const uint8_t* vc = a.v + (int64_t)bg * a.P * (D / 2);
+  const uint32_t* vp = reinterpret_cast<const uint32_t*>(a.v + a.heads_P * (D / 2)) + (int64_t)bg * a.P * (D / 32);
+  for (int blk = blockIdx.x; blk < nblk; blk += gridDim.x) {
+    const int p0 = (base + blk) * kKvBlock;
+    u32x4* kd = ko + ((int64_t)bg * cap + blk) * (4 * D);
+    u32x4* vd = vo + ((int64_t)bg * cap + blk) * (4 * D);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      const int e = i * 256 + threadIdx.x, c = e >> 6, h = (e >> 5) & 1, p = p0 + (e & 31);
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(kc + (int64_t)p * (D / 2) + 8 * c + 4 * h);
+      const uint32_t pr = kp[(int64_t)p * (D / 32) + c / 2];
+      const u32x4 v = k_operand(w, bf16_to_f32(pr & 0xFFFFu) * 512.0f, __uint_as_float(pr & 0xFFFF0000u));
+      kd[e] = p >= j0 && p < len ? v : (u32x4){0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      const int e = i * 256 + threadIdx.x, t = e >> 7, s = (e >> 6) & 1, h = (e >> 5) & 1, m = e & 31;
+      u32x4 o;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int hh = 2 * k + h;  // the layout's lane group: positions 16s + 4hh + r
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(vc + (int64_t)(base + blk) * (16 * D) + (t >> 1) * 1024 +
+                                                              (hh * 16 + (m & 15)) * 16 + (t & 1) * 8 + s * 4);
+        u32x4 pr = *reinterpret_cast<const u32x4*>(vp + (int64_t)(base + blk) * D + t * 32 + hh * 8 + s * 4);
+        float d[4], mm[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int p = p0 + 16 * s + 4 * hh + r;
+          if (p < j0 || p >= len) pr[r] = 0;
+          d[r] = bf16_to_f32(pr[r] & 0xFFFFu);
+          mm[r] = __uint_as_float(pr[r] & 0xFFFF0000u);
+        }
+        const uint2 x = v_operand((m & 16 ? w >> 4 : w) & 0x0F0F0F0Fu, d, mm);
+        o[2 * k] = x.x;
+        o[2 * k + 1] = x.y;
+      }
+      vd[e] = o;
+    }
+  }
+}
+
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// One kilobyte from memory into LDS (16 bytes a lane, lane 0's first).
+__device__ __forceinline__ void copy_lds(const u32x4* src, void* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+
+// Attention of tiles of 32 RW rows (as in kv4_rows_kernel: S^T = K Q^T and
+// O^T = V^T P^T, a lane's row its own) over expanded blocks.  4 waves: RW of
+// them take 32 rows each, times KS that take every KS-th block of 32 positions
+// and are merged at the end.  A step brings KS blocks into LDS, K and V in one
+// buffer each: the next K is requested when the scores are done, the next V
+// when the outputs are, so that each has the other half of the step to arrive.
+//
+// The running maximum is moved only when a score exceeds it by 2^kSlack: the
+// weights then reach 2^kSlack instead of 1, which rounds no differently, and
+// most blocks leave the outputs alone.
+// grid: tiles with the longest ranges first, neighbours of one another on
+// different groups, so that each XCD (workgroups are dealt out to the 8 in
+// turn) works on few groups at a time.
+constexpr float kSlack = 8.0f;
+template <int D, int RW, int KS, int NP>
+__global__ __launch_bounds__(256, 2) void kv4_tiles_kernel(AttnArgs a, const u32x4* __restrict__ kx,
+                                                           const u32x4* __restrict__ vx, int cap, int tiles, int BG) {
+  static_assert(RW * KS == 4, "4 waves");
+  constexpr int NC = D / 16, NT = D / 32, kRows = 32 * RW;
+  constexpr int kVec = 4 * D;  // 16-byte pieces of a block
+  constexpr int kCopies = KS * NC / 4;
+  __shared__ __attribute__((aligned(16))) u32x4 buf[2 * KS * kVec];
+  __shared__ float ms[KS][kRows], ls[KS][kRows];
+  u32x4* const kb = buf;
+  u32x4* const vb = buf + KS * kVec;
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, ks = wave / RW;
+  const int bg = blockIdx.x % BG, tile = tiles - 1 - blockIdx.x / BG, b = bg / a.G, g = bg - b * a.G;
+  const int len = min(max(a.lens[b], 0), a.L), first = len - a.T;  // position of row 0
+
+  const int r0 = tile * kRows + 32 * rw;
+  const int row = r0 + n;
+  const bool there = row < a.rows;
+  const int t = there ? row / a.hg : a.T - 1;
+  const int64_t q_row = ((int64_t)b * a.T + t) * a.H + g * a.hg + (there ? row - t * a.hg : 0);
+  const int row_hi = first + t, row_lo = a.window ? row_hi - a.window + 1 : 0;
+  // Positions of the workgroup's rows, and of the wave's.
+  const int wg_hi = first + min(a.T - 1, (tile * kRows + kRows - 1) / a.hg);
+  const int wg_lo = a.window ? max(0, max(0, first + tile * kRows / a.hg) - a.window + 1) : 0;
+  const int hi_min = first + min(r0 / a.hg, a.T - 1), hi_max = first + min(a.T - 1, (r0 + 31) / a.hg);
+  const int lo_min = a.window ? hi_min - a.window + 1 : 0, lo_max = a.window ? hi_max - a.window + 1 : 0;
+  const int base = first_block(a, len);
+  const int blk0 = wg_lo / kKvBlock, nblk = wg_hi >= wg_lo ? wg_hi / kKvBlock + 1 - blk0 : 0;
+  const u32x4* ksrc = kx + ((int64_t)bg * cap + blk0 - base) * kVec;
+  const u32x4* vsrc = vx + ((int64_t)bg * cap + blk0 - base) * kVec;
+
+  u32x4 qf[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    qf[c] = there ? *reinterpret_cast<const u32x4*>(a.q + q_row * D + 16 * c + 8 * half) : (u32x4){0, 0, 0, 0};
+    if (a.scale2 < 0.0f) qf[c] ^= 0x80008000u;
+  }
+  const float scale2 = fabsf(a.scale2);
+
+  // Blocks past the last are not copied (their waves skip them).
+  const int pieces = nblk * NC;
+  const auto copy = [&](const u32x4* src, u32x4* dst, int step) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int c = step * KS * NC + 4 * i + wave;
+      if (c < pieces) copy_lds(src + (int64_t)c * 64 + lane, dst + (4 * i + wave) * 64);
+    }
+  };
+
+  float m = -INFINITY, l = 0.0f;
+  f32x16 y[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) y[i][e] = 0.0f;
+  const int steps = (nblk + KS - 1) / KS;
+  const auto arrived = [&]() __attribute__((always_inline)) {  // what was requested, and everybody is done with the buffers
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  if (steps > 0) {
+    copy(ksrc, kb, 0);
+    arrived();
+    copy(vsrc, vb, 0);
+  }
+#pragma unroll 1
+  for (int i = 0; i < steps; ++i) {
+    const int blk = i * KS + ks, p0 = (blk0 + blk) * kKvBlock;
+    const bool mine = blk < nblk && p0 <= hi_max && p0 + kKvBlock > lo_min;  // else nothing for the wave's rows
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+    if (mine) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) s = mfma32(kb[ks * kVec + c * 64 + lane], qf[c], s);
+    }
+    arrived();
+    if (i + 1 < steps) copy(ksrc, kb, i + 1);
+    if (mine) {
+      if (p0 < lo_max || p0 + kKvBlock - 1 > hi_min) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int p = p0 + 8 * (e >> 2) + 4 * half + (e & 3);
+          s[e] = p <= row_hi && p >= row_lo ? s[e] : -INFINITY;
+        }
+      }
+      float mx = s[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+      mx = fmaxf(mx, xor_lane<32>(mx)) * scale2;
+      if (__ballot(mx > m + kSlack)) {
+        const float mn = fmaxf(m, mx);
+        const float corr = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+        m = mn;
+        l *= corr;
+#pragma unroll
+        for (int k = 0; k < NT; ++k) y[k] *= corr;
+      }
+      const float mb = m == -INFINITY ? 0.0f : m;
+      u32x4 pf[NP][2];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float f0 = __builtin_amdgcn_exp2f(fmaf(s[2 * e], scale2, -mb)), f1 = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], scale2, -mb));
+        l += f0;
+        l += f1;
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+          const uint32_t w = pack_bf16x2(f0, f1);
+          pf[k][e >> 2][e & 3] = w;
+          f0 -= bf16_to_f32(w & 0xFFFFu);
+          f1 -= __uint_as_float(w & 0xFFFF0000u);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < NT; ++k)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const u32x4 v = vb[ks * kVec + (2 * k + e) * 64 + lane];
+#pragma unroll
+          for (int u = 0; u < NP; ++u) y[k] = mfma32(v, pf[u][e], y[k]);
+        }
+    }
+    arrived();
+    if (i + 1 < steps) copy(vsrc, vb, i + 1);
+  }
+  l += xor_lane<32>(l);
+
+  // The key parts of a row's state, merged into part 0's.
+  if constexpr (KS > 1) {
+    float* ys = reinterpret_cast<float*>(buf);  // [KS - 1][RW][NT][16][64]
+    if (half == 0) {
+      ms[ks][32 * rw + n] = m;
+      ls[ks][32 * rw + n] = l;
+    }
+    if (ks > 0) {
+#pragma unroll
+      for (int k = 0; k < NT; ++k)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) ys[((((ks - 1) * RW + rw) * NT + k) * 16 + e) * 64 + lane] = y[k][e];
+    }
+    __syncthreads();
+    if (ks > 0) return;
+    float mx = m;
+#pragma unroll
+    for (int k = 1; k < KS; ++k) mx = fmaxf(mx, ms[k][32 * rw + n]);
+    const float mb = mx == -INFINITY ? 0.0f : mx;
+    const float c0 = __builtin_amdgcn_exp2f(m - mb);
+    l *= c0;
+#pragma unroll
+    for (int k = 0; k < NT; ++k) y[k] *= c0;
+#pragma unroll
+    for (int u = 1; u < KS; ++u) {
+      const float c = __builtin_amdgcn_exp2f(ms[u][32 * rw + n] - mb);
+      l = fmaf(c, ls[u][32 * rw + n], l);
+#pragma unroll
+      for (int k = 0; k < NT; ++k)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) y[k][e] = fmaf(c, ys[((((u - 1) * RW + rw) * NT + k) * 16 + e) * 64 + lane], y[k][e]);
+    }
+  }
+  if (there) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // a row that attends to nothing is zero
+#pragma unroll
+    for (int k = 0; k < NT; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        put4(a.o, NP == 1, q_row * D + 32 * k + 8 * e + 4 * half,
+             (f32x4){y[k][4 * e] * inv, y[k][4 * e + 1] * inv, y[k][4 * e + 2] * inv, y[k][4 * e + 3] * inv});
+  }
+}
+
+// How a call runs.  Few rows: kv4_rows_kernel, about two workgroups per CU,
+// none with less than a block of positions for each wave at the longest range
+// that the call allows (lengths are known on the device only).  From
+// kTileRows rows of a group on: kv4_expand_kernel and kv4_tiles_kernel.
 constexpr int kAttnGroups = 512;
+constexpr int64_t kTileRows = 96;
 struct AttnPlan {
   int64_t rows, tiles;
-  int splits;
+  int splits;      // of the few rows' launch
+  int rw;          // waves of 32 rows in a tile; 0: few rows
+  int64_t cap;     // expanded blocks of a (sequence, group)
 };
 static AttnPlan attn_plan(int64_t B, int64_t T, int64_t H, int64_t G, int64_t L, int64_t window) {
-  AttnPlan p;
+  AttnPlan p = {};
   p.rows = T * (H / G);
+  p.splits = 1;
+  if (p.rows >= kTileRows) {
+    const int64_t span = window ? std::min(L, window - 1 + T) : L;
+    p.cap = std::min(ceil_div(span, kKvBlock) + 1, kv_positions(L) / kKvBlock);
+    p.rw = B * G * ceil_div(p.rows, 128) >= 512 ? 4 : 2;
+    p.tiles = ceil_div(p.rows, 32 * p.rw);
+    return p;
+  }
   p.tiles = ceil_div(p.rows, kRowTile);
   const int64_t span = window ? std::min(L, window + std::min<int64_t>(T, kRowTile)) : L;
   const int64_t blocks = ceil_div(span, kKvBlock) + 1;
@@ -635,11 +910,29 @@ static AttnPlan attn_plan(int64_t B, int64_t T, int64_t H, int64_t G, int64_t L,
   return p;
 }
 static size_t attn_work_bytes(const AttnPlan& p, int64_t BG, int64_t d) {
+  if (p.rw) return (size_t)(BG * p.cap) * (size_t)(2 * kKvBlock * d * 2);
   return p.splits == 1 ? 0 : (size_t)(BG * p.tiles * p.splits * kRowTile * (d + 4)) * sizeof(float);
+}
+
+template <int D, int RW, int NP>
+static void launch_tiles(const AttnArgs& a, const AttnPlan& p, int64_t BG, hipStream_t stream) {
+  u32x4* kx = reinterpret_cast<u32x4*>(a.work);
+  u32x4* vx = kx + BG * p.cap * (4 * D);
+  hipLaunchKernelGGL((kv4_tiles_kernel<D, RW, 4 / RW, NP>), dim3((unsigned)(BG * p.tiles)), dim3(256), 0, stream, a, kx, vx,
+                     (int)p.cap, (int)p.tiles, (int)BG);
 }
 
 template <int D>
 static void launch_attention(const AttnArgs& a, const AttnPlan& p, int64_t BG, bool bf16, hipStream_t stream) {
+  if (p.rw) {
+    u32x4* kx = reinterpret_cast<u32x4*>(a.work);
+    const int64_t x = std::min(p.cap, std::max<int64_t>(1, kExpandGroups / BG));
+    hipLaunchKernelGGL((kv4_expand_kernel<D>), dim3((unsigned)x, (unsigned)BG), dim3(256), 0, stream, a, kx,
+                       kx + BG * p.cap * (4 * D), (int)p.cap);
+    if (p.rw == 4) bf16 ? launch_tiles<D, 4, 1>(a, p, BG, stream) : launch_tiles<D, 4, 3>(a, p, BG, stream);
+    else bf16 ? launch_tiles<D, 2, 1>(a, p, BG, stream) : launch_tiles<D, 2, 3>(a, p, BG, stream);
+    return;
+  }
   const dim3 grid(p.splits, (unsigned)p.tiles, (unsigned)BG);
   if (bf16) hipLaunchKernelGGL((kv4_rows_kernel<D, 2>), grid, dim3(64 * kAttnWaves), 0, stream, a);
   else hipLaunchKernelGGL((kv4_rows_kernel<D, 3>), grid, dim3(64 * kAttnWaves), 0, stream, a);
@@ -831,7 +1124,10 @@ q4nx_status q4nx_kv4_attention(const uint16_t* d_q, const void* d_k, const void*
   a.rows = (int)p.rows;
   a.hg = (int)(H / G);
   a.splits = p.splits;
+  // A scale of zero (equal weights) becomes the smallest normal one, which
+  // leaves any finite score below 2^-25 but a masked one at -inf.
   a.scale2 = scale * 1.4426950408889634f;
+  if (std::fabs(a.scale2) < 1.17549435e-38f) a.scale2 = 1.17549435e-38f;
   const bool bf16 = o_dtype == Q4NX_BF16;
   if (d == 64) launch_attention<64>(a, p, B * G, bf16, stream);
   else if (d == 128) launch_attention<128>(a, p, B * G, bf16, stream);

@@ -9,7 +9,8 @@ Tolerances (derived, none fitted):
   values, and keys that are neither normed nor rotated: the bytes themselves.
   attention with u = 2^-24: a score is off by at most d u sum|q k| scale + 4 u |s|, so a weight by e = 2 x that (itself and
             the sum) + 2^-20 (exponentials, corrections); the sums over n positions add (n + 64) u; the weights' rounding
-            2^-16 for a bf16 output and 2^-24 for a float32 one: e' sum p|v|.  Then the output's rounding.
+            2^-24 for a float32 output; for a bf16 one 2^-16 with few rows (two bf16 terms) and 2^-8 with many (one term:
+            half a step of bf16, as the output's own rounding): e' sum p|v|.  Then the output's rounding.
 """
 import numpy as np
 import pytest
@@ -290,7 +291,8 @@ def _check_attention(q4, H, G, d, lens, T, window, bf16, L=None, scale=None, see
     for b in range(B):
         ref, bound, dots = kv4.attention(q[b], K[b], V[b], lens[b], window, scale)
         ds = abs(scale) * dots * (d * U + 4 * U)
-        e = 2 * ds + 2.0 ** -20 + (lens[b] + 64) * U + (2.0 ** -16 if bf16 else 2.0 ** -24)
+        rounding = 2.0 ** -24 if not bf16 else 2.0 ** -16 if T * H // G < 96 else 2.0 ** -8
+        e = 2 * ds + 2.0 ** -20 + (lens[b] + 64) * U + rounding
         tol = e * bound + (2.0 ** -8 if bf16 else U) * np.abs(ref) + 1e-37
         err = np.abs(got[b] - ref)
         worst = max(worst, float((err / tol).max()))
@@ -327,6 +329,18 @@ def _check_attention(q4, H, G, d, lens, T, window, bf16, L=None, scale=None, see
     (3, 1, 128, [300], 130, 17, False, 512),
     (16, 16, 64, [120], 120, 0, True, 120),
     (16, 1, 64, [90], 90, 40, False, 90),
+    # many rows: tiles of 64 rows (two key parts) and, from 512 of them on, of 128; a tile's last rows missing; a
+    # sequence shorter than its rows, and an empty one; windows that leave whole blocks of a tile to some rows only
+    (8, 4, 128, [333], 100, 0, False, 400),
+    (8, 4, 256, [333], 333, 0, True, 333),
+    (12, 4, 64, [700, 40, 0], 64, 0, False, 701),
+    (4, 2, 64, [513], 257, 100, False, 600),
+    (4, 2, 128, [513], 257, 1, True, 600),
+    (64, 64, 64, [100, 96, 200, 5, 97, 0, 128, 129], 96, 0, False, 200),
+    (64, 64, 64, [100, 96, 200, 5, 97, 0, 128, 129], 96, 0, True, 200),
+    (64, 64, 128, [100, 96, 120, 5, 97, 0, 128, 129], 96, 50, False, 129),
+    (64, 64, 256, [100, 96, 20, 5, 97, 0, 98, 99], 96, 0, False, 100),
+    (64, 64, 256, [100, 96, 20, 5, 97, 0, 98, 99], 96, 33, True, 100),
 ])
 def test_attention(q4, H, G, d, lens, T, window, bf16, L):
     _check_attention(q4, H, G, d, lens, T, window, bf16, L)
@@ -336,6 +350,25 @@ def test_attention_peaked_and_flat(q4):
     _check_attention(q4, 4, 2, 128, [400], 1, 0, False, 400, spread=20.0)
     _check_attention(q4, 4, 2, 128, [400], 3, 0, False, 400, scale=-0.3)
     _check_attention(q4, 4, 2, 128, [400], 1, 0, False, 400, scale=1e-6)
+    for T in (3, 100):                                                    # few rows and many
+        _check_attention(q4, 4, 2, 128, [400], T, 0, False, 400, scale=-0.3)
+        _check_attention(q4, 4, 2, 128, [400], T, 30, False, 400, scale=1e-30)
+        _check_attention(q4, 4, 2, 128, [400], T, 0, False, 400, spread=20.0)
+
+
+def test_attention_scale_zero_is_the_mean(q4):
+    print("[case] scale 0", flush=True)
+    rng = np.random.default_rng(4)
+    H, G, d, n = 4, 2, 64, 130
+    caches, (K, V) = _cache(rng, q4, 1, G, d, n, [n])
+    for T in (2, 60):
+        q = _bf16(oracle.f32_to_bf16(rng.standard_normal((1, T, H, d)).astype(np.float32)))
+        o = torch.full((1, T, H, d), float("nan"), device="cuda")
+        q4.q4nx_kv4_attention(q, *caches, _ints([n]), 1, T, H, G, d, n, 40, 0.0, o,
+                              torch.empty(q4.q4nx_kv4_workspace_size(1, T, H, G, d, n, 40) + 16, dtype=torch.uint8, device="cuda"))
+        v = oracle.bf16_to_f32(V[0]).astype(np.float64)
+        ref = np.stack([v[:, p - 39:p + 1].mean(1) for p in range(n - T, n)])              # [T][G][d]
+        assert np.allclose(o[0].cpu().numpy(), np.repeat(ref, H // G, 1), rtol=0, atol=6 * (n + 64) * U)
 
 
 def test_attention_lengths_are_clamped(q4):
