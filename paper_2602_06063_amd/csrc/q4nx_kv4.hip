@@ -695,11 +695,14 @@ __device__ __forceinline__ void copy_lds(const u32x4* src, void* dst) {
 }
 
 // Attention of tiles of 32 RW rows (as in kv4_rows_kernel: S^T = K Q^T and
-// O^T = V^T P^T, a lane's row its own) over expanded blocks.  4 waves: RW of
-// them take 32 rows each, times KS that take every KS-th block of 32 positions
-// and are merged at the end.  A step brings KS blocks into LDS, K and V in one
-// buffer each: the next K is requested when the scores are done, the next V
-// when the outputs are, so that each has the other half of the step to arrive.
+// O^T = V^T P^T, a lane's row its own) over expanded blocks.  RW KS waves: RW
+// of them take 32 rows each, times KS that take every KS-th block of 32
+// positions and are merged at the end.  A step brings KS blocks into LDS.
+//   KS = 1  two buffers: a step's blocks are requested a step ahead, and one
+//           barrier a step says that they are there and that the others are free
+//   KS > 1  one buffer each for K and V: the next K is requested when the
+//           scores are done, the next V when the outputs are, so that each has
+//           the other half of the step to arrive
 //
 // The running maximum is moved only when a score exceeds it by 2^kSlack: the
 // weights then reach 2^kSlack instead of 1, which rounds no differently, and
@@ -709,20 +712,21 @@ __device__ __forceinline__ void copy_lds(const u32x4* src, void* dst) {
 // turn) works on few groups at a time.
 constexpr float kSlack = 8.0f;
 template <int D, int RW, int KS, int NP>
-__global__ __launch_bounds__(256, 2) void kv4_tiles_kernel(AttnArgs a, const u32x4* __restrict__ kx,
-                                                           const u32x4* __restrict__ vx, int cap, int tiles, int BG) {
-  static_assert(RW * KS == 4, "4 waves");
-  constexpr int NC = D / 16, NT = D / 32, kRows = 32 * RW;
+__global__ __launch_bounds__(64 * RW * KS, 2) void kv4_tiles_kernel(AttnArgs a, const u32x4* __restrict__ kx,
+                                                                    const u32x4* __restrict__ vx, int cap, int tiles,
+                                                                    int BG) {
+  constexpr int W = RW * KS, NC = D / 16, NT = D / 32, kRows = 32 * RW;
   constexpr int kVec = 4 * D;  // 16-byte pieces of a block
-  constexpr int kCopies = KS * NC / 4;
-  __shared__ __attribute__((aligned(16))) u32x4 buf[2 * KS * kVec];
+  constexpr int kCopies = KS * NC / W;
+  constexpr bool kRing = KS == 1;
+  constexpr int kAhead = D == 128 ? 8 : 4;  // operands read from LDS before their products begin (more would spill at 256)
+  static_assert(KS * NC % W == 0, "every wave copies as much");
+  __shared__ __attribute__((aligned(16))) u32x4 buf[2 * (kRing ? 2 : KS) * kVec];
   __shared__ float ms[KS][kRows], ls[KS][kRows];
-  u32x4* const kb = buf;
-  u32x4* const vb = buf + KS * kVec;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, ks = wave / RW;
   const int bg = blockIdx.x % BG, tile = tiles - 1 - blockIdx.x / BG, b = bg / a.G, g = bg - b * a.G;
-  const int len = min(max(a.lens[b], 0), a.L), first = len - a.T;  // position of row 0
+  const int len = __builtin_amdgcn_readfirstlane(min(max(a.lens[b], 0), a.L)), first = len - a.T;  // position of row 0
 
   const int r0 = tile * kRows + 32 * rw;
   const int row = r0 + n;
@@ -737,8 +741,8 @@ __global__ __launch_bounds__(256, 2) void kv4_tiles_kernel(AttnArgs a, const u32
   const int lo_min = a.window ? hi_min - a.window + 1 : 0, lo_max = a.window ? hi_max - a.window + 1 : 0;
   const int base = first_block(a, len);
   const int blk0 = wg_lo / kKvBlock, nblk = wg_hi >= wg_lo ? wg_hi / kKvBlock + 1 - blk0 : 0;
-  const u32x4* ksrc = kx + ((int64_t)bg * cap + blk0 - base) * kVec;
-  const u32x4* vsrc = vx + ((int64_t)bg * cap + blk0 - base) * kVec;
+  const u32x4* ksrc = kx + ((int64_t)bg * cap + blk0 - base) * kVec + lane;
+  const u32x4* vsrc = vx + ((int64_t)bg * cap + blk0 - base) * kVec + lane;
 
   u32x4 qf[NC];
 #pragma unroll
@@ -753,9 +757,13 @@ __global__ __launch_bounds__(256, 2) void kv4_tiles_kernel(AttnArgs a, const u32
   const auto copy = [&](const u32x4* src, u32x4* dst, int step) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
-      const int c = step * KS * NC + 4 * i + wave;
-      if (c < pieces) copy_lds(src + (int64_t)c * 64 + lane, dst + (4 * i + wave) * 64);
+      const int c = step * KS * NC + W * i + wave;
+      if (KS == 1 || c < pieces) copy_lds(src + (int64_t)c * 64, dst + (W * i + wave) * 64);
     }
+  };
+  const auto arrived = [&]() __attribute__((always_inline)) {  // what was requested, and everybody is done with the buffers
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
   };
 
   float m = -INFINITY, l = 0.0f;
@@ -765,29 +773,51 @@ __global__ __launch_bounds__(256, 2) void kv4_tiles_kernel(AttnArgs a, const u32
 #pragma unroll
     for (int e = 0; e < 16; ++e) y[i][e] = 0.0f;
   const int steps = (nblk + KS - 1) / KS;
-  const auto arrived = [&]() __attribute__((always_inline)) {  // what was requested, and everybody is done with the buffers
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-  };
   if (steps > 0) {
-    copy(ksrc, kb, 0);
-    arrived();
-    copy(vsrc, vb, 0);
+    copy(ksrc, buf, 0);
+    if constexpr (kRing) {
+      copy(vsrc, buf + kVec, 0);
+    } else {
+      arrived();
+      copy(vsrc, buf + KS * kVec, 0);
+    }
   }
 #pragma unroll 1
   for (int i = 0; i < steps; ++i) {
     const int blk = i * KS + ks, p0 = (blk0 + blk) * kKvBlock;
     const bool mine = blk < nblk && p0 <= hi_max && p0 + kKvBlock > lo_min;  // else nothing for the wave's rows
+    const u32x4* const kb = (kRing ? buf + (i & 1) * 2 * kVec : buf + ks * kVec) + lane;
+    const u32x4* const vb = (kRing ? buf + ((i & 1) * 2 + 1) * kVec : buf + (KS + ks) * kVec) + lane;
+    if constexpr (kRing) {
+      arrived();
+      if (i + 1 < steps) {
+        copy(ksrc, buf + ((i + 1) & 1) * 2 * kVec, i + 1);
+        copy(vsrc, buf + (((i + 1) & 1) * 2 + 1) * kVec, i + 1);
+      }
+    }
     f32x16 s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.0f;
     if (mine) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) s = mfma32(kb[ks * kVec + c * 64 + lane], qf[c], s);
+      for (int c0 = 0; c0 < NC; c0 += kAhead) {
+        u32x4 kf[kAhead];
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c) kf[c] = kb[(c0 + c) * 64];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c) s = mfma32(kf[c], qf[c0 + c], s);
+      }
     }
-    arrived();
-    if (i + 1 < steps) copy(ksrc, kb, i + 1);
+    if constexpr (!kRing) {
+      arrived();
+      if (i + 1 < steps) copy(ksrc, buf, i + 1);
+    }
     if (mine) {
+      u32x4 vf[kAhead];  // operand (value tile k, half e of the positions) at 2k + e
+#pragma unroll
+      for (int c = 0; c < kAhead; ++c) vf[c] = vb[c * 64];
+      __builtin_amdgcn_sched_barrier(0);
       if (p0 < lo_max || p0 + kKvBlock - 1 > hi_min) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -809,11 +839,12 @@ __global__ __launch_bounds__(256, 2) void kv4_tiles_kernel(AttnArgs a, const u32
       }
       const float mb = m == -INFINITY ? 0.0f : m;
       u32x4 pf[NP][2];
+      float l2 = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float f0 = __builtin_amdgcn_exp2f(fmaf(s[2 * e], scale2, -mb)), f1 = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], scale2, -mb));
         l += f0;
-        l += f1;
+        l2 += f1;
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
           const uint32_t w = pack_bf16x2(f0, f1);
@@ -822,52 +853,61 @@ __global__ __launch_bounds__(256, 2) void kv4_tiles_kernel(AttnArgs a, const u32
           f1 -= __uint_as_float(w & 0xFFFF0000u);
         }
       }
+      l += l2;
 #pragma unroll
-      for (int k = 0; k < NT; ++k)
+      for (int c0 = 0; c0 < NC; c0 += kAhead) {
+        // Both halves of the positions tile by tile would be chains of two.
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const u32x4 v = vb[ks * kVec + (2 * k + e) * 64 + lane];
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int u = 0; u < NP; ++u) y[k] = mfma32(v, pf[u][e], y[k]);
+          for (int u = 0; u < NP; ++u)
+#pragma unroll
+            for (int k = 0; k < kAhead / 2; ++k) y[c0 / 2 + k] = mfma32(vf[2 * k + e], pf[u][e], y[c0 / 2 + k]);
+        if (c0 + kAhead < NC) {
+#pragma unroll
+          for (int c = 0; c < kAhead; ++c) vf[c] = vb[(c0 + kAhead + c) * 64];
         }
+      }
     }
-    arrived();
-    if (i + 1 < steps) copy(vsrc, vb, i + 1);
+    if constexpr (!kRing) {
+      arrived();
+      if (i + 1 < steps) copy(vsrc, buf + KS * kVec, i + 1);
+    }
   }
   l += xor_lane<32>(l);
 
-  // The key parts of a row's state, merged into part 0's.
+  // The key parts of a row's state, merged by halves into part 0's: the upper
+  // half leaves its states in the buffers (as large as half the parts need).
   if constexpr (KS > 1) {
-    float* ys = reinterpret_cast<float*>(buf);  // [KS - 1][RW][NT][16][64]
-    if (half == 0) {
-      ms[ks][32 * rw + n] = m;
-      ls[ks][32 * rw + n] = l;
-    }
-    if (ks > 0) {
+    static_assert(sizeof(buf) >= sizeof(float) * (KS / 2) * RW * NT * 16 * 64, "the states of half the parts");
+    float* const ys = reinterpret_cast<float*>(buf) + lane;
 #pragma unroll
-      for (int k = 0; k < NT; ++k)
+    for (int s = KS / 2; s >= 1; s /= 2) {
+      float* const mine = ys + ((ks >= s ? ks - s : ks) * RW + rw) * (NT * 16 * 64);
+      if (ks >= s && ks < 2 * s) {
+        if (half == 0) {
+          ms[ks][32 * rw + n] = m;
+          ls[ks][32 * rw + n] = l;
+        }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) ys[((((ks - 1) * RW + rw) * NT + k) * 16 + e) * 64 + lane] = y[k][e];
+        for (int k = 0; k < NT; ++k)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) mine[(k * 16 + e) * 64] = y[k][e];
+      }
+      __syncthreads();
+      if (ks < s) {
+        const float m1 = ms[ks + s][32 * rw + n], mx = fmaxf(m, m1), mb = mx == -INFINITY ? 0.0f : mx;
+        const float c0 = __builtin_amdgcn_exp2f(m - mb), c1 = __builtin_amdgcn_exp2f(m1 - mb);
+        m = mx;
+        l = fmaf(c1, ls[ks + s][32 * rw + n], c0 * l);
+#pragma unroll
+        for (int k = 0; k < NT; ++k)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) y[k][e] = fmaf(c1, mine[(k * 16 + e) * 64], c0 * y[k][e]);
+      }
+      __syncthreads();
     }
-    __syncthreads();
     if (ks > 0) return;
-    float mx = m;
-#pragma unroll
-    for (int k = 1; k < KS; ++k) mx = fmaxf(mx, ms[k][32 * rw + n]);
-    const float mb = mx == -INFINITY ? 0.0f : mx;
-    const float c0 = __builtin_amdgcn_exp2f(m - mb);
-    l *= c0;
-#pragma unroll
-    for (int k = 0; k < NT; ++k) y[k] *= c0;
-#pragma unroll
-    for (int u = 1; u < KS; ++u) {
-      const float c = __builtin_amdgcn_exp2f(ms[u][32 * rw + n] - mb);
-      l = fmaf(c, ls[u][32 * rw + n], l);
-#pragma unroll
-      for (int k = 0; k < NT; ++k)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) y[k][e] = fmaf(c, ys[((((u - 1) * RW + rw) * NT + k) * 16 + e) * 64 + lane], y[k][e]);
-    }
   }
   if (there) {
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // a row that attends to nothing is zero
@@ -914,12 +954,12 @@ static size_t attn_work_bytes(const AttnPlan& p, int64_t BG, int64_t d) {
   return p.splits == 1 ? 0 : (size_t)(BG * p.tiles * p.splits * kRowTile * (d + 4)) * sizeof(float);
 }
 
-template <int D, int RW, int NP>
+template <int D, int RW, int KS, int NP>
 static void launch_tiles(const AttnArgs& a, const AttnPlan& p, int64_t BG, hipStream_t stream) {
   u32x4* kx = reinterpret_cast<u32x4*>(a.work);
   u32x4* vx = kx + BG * p.cap * (4 * D);
-  hipLaunchKernelGGL((kv4_tiles_kernel<D, RW, 4 / RW, NP>), dim3((unsigned)(BG * p.tiles)), dim3(256), 0, stream, a, kx, vx,
-                     (int)p.cap, (int)p.tiles, (int)BG);
+  hipLaunchKernelGGL((kv4_tiles_kernel<D, RW, KS, NP>), dim3((unsigned)(BG * p.tiles)), dim3(64 * RW * KS), 0, stream, a,
+                     kx, vx, (int)p.cap, (int)p.tiles, (int)BG);
 }
 
 template <int D>
@@ -929,8 +969,8 @@ static void launch_attention(const AttnArgs& a, const AttnPlan& p, int64_t BG, b
     const int64_t x = std::min(p.cap, std::max<int64_t>(1, kExpandGroups / BG));
     hipLaunchKernelGGL((kv4_expand_kernel<D>), dim3((unsigned)x, (unsigned)BG), dim3(256), 0, stream, a, kx,
                        kx + BG * p.cap * (4 * D), (int)p.cap);
-    if (p.rw == 4) bf16 ? launch_tiles<D, 4, 1>(a, p, BG, stream) : launch_tiles<D, 4, 3>(a, p, BG, stream);
-    else bf16 ? launch_tiles<D, 2, 1>(a, p, BG, stream) : launch_tiles<D, 2, 3>(a, p, BG, stream);
+    if (p.rw == 4) bf16 ? launch_tiles<D, 4, 1, 1>(a, p, BG, stream) : launch_tiles<D, 4, 1, 3>(a, p, BG, stream);
+    else bf16 ? launch_tiles<D, 2, 4, 1>(a, p, BG, stream) : launch_tiles<D, 2, 4, 3>(a, p, BG, stream);
     return;
   }
   const dim3 grid(p.splits, (unsigned)p.tiles, (unsigned)BG);
