@@ -688,21 +688,24 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// One kilobyte from memory into LDS (16 bytes a lane, lane 0's first).
-__device__ __forceinline__ void copy_lds(const u32x4* src, void* dst) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+// One kilobyte from memory (a wave's own address, lane l's 16 bytes at 16 l,
+// which `lane16` holds) into LDS at byte `lds`.  As assembly, since the
+// compiler lets every later read of LDS wait for every such copy; the wait is
+// `arrived` below.  (It loads no registers; nothing else here uses M0, and the
+// idle step is what M0 needs before its use.)
+__device__ __forceinline__ void copy_lds(const u32x4* src, uint32_t lane16, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(lane16), "s"(src), "s"(lds));
 }
 
 // Attention of tiles of 32 RW rows (as in kv4_rows_kernel: S^T = K Q^T and
 // O^T = V^T P^T, a lane's row its own) over expanded blocks.  RW KS waves: RW
 // of them take 32 rows each, times KS that take every KS-th block of 32
-// positions and are merged at the end.  A step brings KS blocks into LDS.
-//   KS = 1  two buffers: a step's blocks are requested a step ahead, and one
-//           barrier a step says that they are there and that the others are free
-//   KS > 1  one buffer each for K and V: the next K is requested when the
-//           scores are done, the next V when the outputs are, so that each has
-//           the other half of the step to arrive
+// positions and are merged at the end.  A step brings KS blocks into LDS, into
+// the other of two buffers than the one in use, and one barrier a step says
+// that they are there.  A wave forms the scores of its next block while it
+// takes the exponentials of this one, so that the matrix unit works under the
+// vector unit's share of the step: K is a step ahead of V.
 //
 // The running maximum is moved only when a score exceeds it by 2^kSlack: the
 // weights then reach 2^kSlack instead of 1, which rounds no differently, and
@@ -711,17 +714,31 @@ __device__ __forceinline__ void copy_lds(const u32x4* src, void* dst) {
 // different groups, so that each XCD (workgroups are dealt out to the 8 in
 // turn) works on few groups at a time.
 constexpr float kSlack = 8.0f;
+
+// Orders what stands between scheduling barriers: N times a matrix
+// instruction, V vector ones that run under it, a read of LDS and a copy into it
+// (copies in a row hold their wave up, 16 clocks each).
+template <int N, int V>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 template <int D, int RW, int KS, int NP>
-__global__ __launch_bounds__(64 * RW * KS, 2) void kv4_tiles_kernel(AttnArgs a, const u32x4* __restrict__ kx,
-                                                                    const u32x4* __restrict__ vx, int cap, int tiles,
-                                                                    int BG) {
+__global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kernel(AttnArgs a, const u32x4* __restrict__ kx,
+                                                                                   const u32x4* __restrict__ vx, int cap,
+                                                                                   int tiles, int BG) {
   constexpr int W = RW * KS, NC = D / 16, NT = D / 32, kRows = 32 * RW;
   constexpr int kVec = 4 * D;  // 16-byte pieces of a block
   constexpr int kCopies = KS * NC / W;
-  constexpr bool kRing = KS == 1;
-  constexpr int kAhead = D == 128 ? 8 : 4;  // operands read from LDS before their products begin (more would spill at 256)
+  constexpr int kAhead = NC < 8 ? NC : 8;  // V's operands read from LDS before their products begin
   static_assert(KS * NC % W == 0, "every wave copies as much");
-  __shared__ __attribute__((aligned(16))) u32x4 buf[2 * (kRing ? 2 : KS) * kVec];
+  __shared__ __attribute__((aligned(16))) u32x4 buf[4 * KS * kVec];  // K, V of even steps; of odd ones
   __shared__ float ms[KS][kRows], ls[KS][kRows];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, ks = wave / RW;
@@ -734,15 +751,15 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void kv4_tiles_kernel(AttnArgs a, 
   const int t = there ? row / a.hg : a.T - 1;
   const int64_t q_row = ((int64_t)b * a.T + t) * a.H + g * a.hg + (there ? row - t * a.hg : 0);
   const int row_hi = first + t, row_lo = a.window ? row_hi - a.window + 1 : 0;
-  // Positions of the workgroup's rows, and of the wave's.
-  const int wg_hi = first + min(a.T - 1, (tile * kRows + kRows - 1) / a.hg);
-  const int wg_lo = a.window ? max(0, max(0, first + tile * kRows / a.hg) - a.window + 1) : 0;
-  const int hi_min = first + min(r0 / a.hg, a.T - 1), hi_max = first + min(a.T - 1, (r0 + 31) / a.hg);
-  const int lo_min = a.window ? hi_min - a.window + 1 : 0, lo_max = a.window ? hi_max - a.window + 1 : 0;
-  const int base = first_block(a, len);
+  // Positions of the workgroup's rows, and what all the wave's rows see.
+  const int wg_hi = __builtin_amdgcn_readfirstlane(first + min(a.T - 1, (tile * kRows + kRows - 1) / a.hg));
+  const int wg_lo = __builtin_amdgcn_readfirstlane(a.window ? max(0, max(0, first + tile * kRows / a.hg) - a.window + 1) : 0);
+  const int hi_min = __builtin_amdgcn_readfirstlane(first + min(r0 / a.hg, a.T - 1));
+  const int lo_max = __builtin_amdgcn_readfirstlane(a.window ? first + min(a.T - 1, (r0 + 31) / a.hg) - a.window + 1 : 0);
+  const int base = __builtin_amdgcn_readfirstlane(first_block(a, len));
   const int blk0 = wg_lo / kKvBlock, nblk = wg_hi >= wg_lo ? wg_hi / kKvBlock + 1 - blk0 : 0;
-  const u32x4* ksrc = kx + ((int64_t)bg * cap + blk0 - base) * kVec + lane;
-  const u32x4* vsrc = vx + ((int64_t)bg * cap + blk0 - base) * kVec + lane;
+  const u32x4* ksrc = kx + ((int64_t)bg * cap + blk0 - base) * kVec;
+  const u32x4* vsrc = vx + ((int64_t)bg * cap + blk0 - base) * kVec;
 
   u32x4 qf[NC];
 #pragma unroll
@@ -752,129 +769,156 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void kv4_tiles_kernel(AttnArgs a, 
   }
   const float scale2 = fabsf(a.scale2);
 
-  // Blocks past the last are not copied (their waves skip them).
-  const int pieces = nblk * NC;
-  const auto copy = [&](const u32x4* src, u32x4* dst, int step) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i) {
-      const int c = step * KS * NC + W * i + wave;
-      if (KS == 1 || c < pieces) copy_lds(src + (int64_t)c * 64, dst + (W * i + wave) * 64);
-    }
+  // In place of pieces past the last block, the last piece (every wave copies
+  // as often, so that it can wait for the older of two batches); positions past
+  // the rows' own are masked like all that a row does not see.
+  const int last = nblk * NC - 1;
+  const uint32_t buf_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)buf;
+  const auto copy_piece = [&](const u32x4* src, int which, int step, int i) __attribute__((always_inline)) {
+    copy_lds(src + (int64_t)min(step * KS * NC + W * i + wave, last) * 64, 16 * lane,
+             buf_lds + (((step & 1) * 2 + which) * (KS * kVec) + (W * i + wave) * 64) * 16);
   };
-  const auto arrived = [&]() __attribute__((always_inline)) {  // what was requested, and everybody is done with the buffers
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+  const auto copy = [&](const u32x4* src, int which, int step) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) copy_piece(src, which, step, i);
+  };
+  // All but the newest two of the copies have arrived, and every wave has read
+  // what it asked LDS for.  (A barrier of the language would wait for all.)
+  const auto arrived = [&]() __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kCopies) : "memory");
+  };
+  const auto operands = [&](int which, int step) __attribute__((always_inline)) {
+    return buf + ((step & 1) * 2 + which) * (KS * kVec) + ks * kVec + lane;
   };
 
   float m = -INFINITY, l = 0.0f;
-  f32x16 y[NT];
+  f32x16 y[NT], s, s2;
 #pragma unroll
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) y[i][e] = 0.0f;
   const int steps = (nblk + KS - 1) / KS;
+  u32x4 kf[NC];  // K's operands of the next step
   if (steps > 0) {
-    copy(ksrc, buf, 0);
-    if constexpr (kRing) {
-      copy(vsrc, buf + kVec, 0);
-    } else {
-      arrived();
-      copy(vsrc, buf + KS * kVec, 0);
-    }
-  }
-#pragma unroll 1
-  for (int i = 0; i < steps; ++i) {
-    const int blk = i * KS + ks, p0 = (blk0 + blk) * kKvBlock;
-    const bool mine = blk < nblk && p0 <= hi_max && p0 + kKvBlock > lo_min;  // else nothing for the wave's rows
-    const u32x4* const kb = (kRing ? buf + (i & 1) * 2 * kVec : buf + ks * kVec) + lane;
-    const u32x4* const vb = (kRing ? buf + ((i & 1) * 2 + 1) * kVec : buf + (KS + ks) * kVec) + lane;
-    if constexpr (kRing) {
-      arrived();
-      if (i + 1 < steps) {
-        copy(ksrc, buf + ((i + 1) & 1) * 2 * kVec, i + 1);
-        copy(vsrc, buf + (((i + 1) & 1) * 2 + 1) * kVec, i + 1);
-      }
-    }
-    f32x16 s;
+    copy(ksrc, 0, 0);
+    copy(ksrc, 0, 1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const u32x4* const k0 = operands(0, 0);
+    const u32x4* const k1 = operands(0, 1);
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.0f;
-    if (mine) {
 #pragma unroll
-      for (int c0 = 0; c0 < NC; c0 += kAhead) {
-        u32x4 kf[kAhead];
+    for (int c = 0; c < NC; ++c) s = mfma32(k0[c * 64], qf[c], s);
 #pragma unroll
-        for (int c = 0; c < kAhead; ++c) kf[c] = kb[(c0 + c) * 64];
-        __builtin_amdgcn_sched_barrier(0);
+    for (int c = 0; c < NC; ++c) kf[c] = k1[c * 64];
+    __syncthreads();
+    copy(ksrc, 0, 2);
+    copy(vsrc, 1, 0);
+    copy(ksrc, 0, 3);
+  }
+  // Step i: the weights and outputs of scores s, and the scores sn of the next
+  // step (of the last step: of whatever is there) from kf, which takes K of
+  // step i + 2 meanwhile.  A copy is asked for as soon as every wave is done
+  // with its place, K's in the middle of a step and V's at its beginning, and
+  // has a step and a half to arrive: three copies are under way at a time.
+  const auto step = [&](int i, f32x16& s, f32x16& sn) __attribute__((always_inline)) {
+    const int p0 = (blk0 + i * KS + ks) * kKvBlock;
+    const u32x4* const k2 = operands(0, i + 2);
+    const u32x4* const vb = operands(1, i);
+    arrived();  // K of step i + 2
+    if (p0 < lo_max || p0 + kKvBlock - 1 > hi_min) {
 #pragma unroll
-        for (int c = 0; c < kAhead; ++c) s = mfma32(kf[c], qf[c0 + c], s);
+      for (int e = 0; e < 16; ++e) {
+        const int p = p0 + 8 * (e >> 2) + 4 * half + (e & 3);
+        s[e] = p <= row_hi && p >= row_lo ? s[e] : -INFINITY;
       }
     }
-    if constexpr (!kRing) {
-      arrived();
-      if (i + 1 < steps) copy(ksrc, buf, i + 1);
+    // The next scores, half with this block's maximum, half with the first half
+    // of its weights.
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sn[e] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NC / 2; ++c) {
+      sn = mfma32(kf[c], qf[c], sn);
+      kf[c] = k2[c * 64];
+      if (c < kCopies) copy_piece(vsrc, 1, i + 1, c);
     }
-    if (mine) {
-      u32x4 vf[kAhead];  // operand (value tile k, half e of the positions) at 2k + e
+    float mx = s[0];
 #pragma unroll
-      for (int c = 0; c < kAhead; ++c) vf[c] = vb[c * 64];
-      __builtin_amdgcn_sched_barrier(0);
-      if (p0 < lo_max || p0 + kKvBlock - 1 > hi_min) {
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+    mx = fmaxf(mx, xor_lane<32>(mx)) * scale2;
+    const bool move = __ballot(mx > m + kSlack) != 0;
+    interleave<NC / 2, 40 / NC>();
+    if (move) {
+      const float mn = fmaxf(m, mx);
+      const float corr = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+      m = mn;
+      l *= corr;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int p = p0 + 8 * (e >> 2) + 4 * half + (e & 3);
-          s[e] = p <= row_hi && p >= row_lo ? s[e] : -INFINITY;
-        }
-      }
-      float mx = s[0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
-      mx = fmaxf(mx, xor_lane<32>(mx)) * scale2;
-      if (__ballot(mx > m + kSlack)) {
-        const float mn = fmaxf(m, mx);
-        const float corr = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
-        m = mn;
-        l *= corr;
-#pragma unroll
-        for (int k = 0; k < NT; ++k) y[k] *= corr;
-      }
-      const float mb = m == -INFINITY ? 0.0f : m;
-      u32x4 pf[NP][2];
+      for (int k = 0; k < NT; ++k) y[k] *= corr;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const float mb = m == -INFINITY ? 0.0f : m;
+    u32x4 pf[NP][2];
+    const auto weights = [&](int h) __attribute__((always_inline)) {
       float l2 = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float f0 = __builtin_amdgcn_exp2f(fmaf(s[2 * e], scale2, -mb)), f1 = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], scale2, -mb));
+      for (int e = 0; e < 4; ++e) {
+        float f0 = __builtin_amdgcn_exp2f(fmaf(s[8 * h + 2 * e], scale2, -mb));
+        float f1 = __builtin_amdgcn_exp2f(fmaf(s[8 * h + 2 * e + 1], scale2, -mb));
         l += f0;
         l2 += f1;
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
           const uint32_t w = pack_bf16x2(f0, f1);
-          pf[k][e >> 2][e & 3] = w;
+          pf[k][h][e] = w;
           f0 -= bf16_to_f32(w & 0xFFFFu);
           f1 -= __uint_as_float(w & 0xFFFF0000u);
         }
       }
       l += l2;
+    };
 #pragma unroll
-      for (int c0 = 0; c0 < NC; c0 += kAhead) {
-        // Both halves of the positions tile by tile would be chains of two.
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int u = 0; u < NP; ++u)
-#pragma unroll
-            for (int k = 0; k < kAhead / 2; ++k) y[c0 / 2 + k] = mfma32(vf[2 * k + e], pf[u][e], y[c0 / 2 + k]);
-        if (c0 + kAhead < NC) {
-#pragma unroll
-          for (int c = 0; c < kAhead; ++c) vf[c] = vb[(c0 + kAhead + c) * 64];
-        }
-      }
+    for (int c = NC / 2; c < NC; ++c) {
+      sn = mfma32(kf[c], qf[c], sn);
+      kf[c] = k2[c * 64];
     }
-    if constexpr (!kRing) {
-      arrived();
-      if (i + 1 < steps) copy(vsrc, buf + KS * kVec, i + 1);
+    weights(0);
+    interleave<NC / 2, 80 / NC>();
+    arrived();  // V of step i
+    // The last step may have no block for this part of the keys (and the
+    // copies of it and of the one before it nobody reads).
+    if (KS > 1 && i * KS + ks >= nblk) return;
+    __builtin_amdgcn_sched_barrier(0);
+    // The outputs, value tiles of half e of the positions after the other (one
+    // tile's two halves would be a chain), operands read kAhead tiles before;
+    // the other weights under the first of them.
+    u32x4 vf[kAhead];
+#pragma unroll
+    for (int c = 0; c < kAhead; ++c) vf[c] = vb[(2 * (c % NT) + c / NT) * 64];
+    weights(1);
+#pragma unroll
+    for (int c = 0; c < 2 * NT; ++c) {
+#pragma unroll
+      for (int u = 0; u < NP; ++u) y[c % NT] = mfma32(vf[c % kAhead], pf[u][c / NT], y[c % NT]);
+      if (c < kCopies) copy_piece(ksrc, 0, i + 4, c);
+      const int r = c + kAhead;
+      if (r < 2 * NT) vf[c % kAhead] = vb[(2 * (r % NT) + r / NT) * 64];
     }
+    __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+    interleave<NC, 80 / NC>();
+  };
+#pragma unroll 1
+  for (int i = 0; i < steps; i += 2) {
+    step(i, s, s2);
+    if (i + 1 < steps) step(i + 1, s2, s);
   }
   l += xor_lane<32>(l);
+  // Nothing is under way into LDS when the merge below takes the buffers, or the workgroup ends.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
 
   // The key parts of a row's state, merged by halves into part 0's: the upper
   // half leaves its states in the buffers (as large as half the parts need).
@@ -970,7 +1014,7 @@ static void launch_attention(const AttnArgs& a, const AttnPlan& p, int64_t BG, b
     hipLaunchKernelGGL((kv4_expand_kernel<D>), dim3((unsigned)x, (unsigned)BG), dim3(256), 0, stream, a, kx,
                        kx + BG * p.cap * (4 * D), (int)p.cap);
     if (p.rw == 4) bf16 ? launch_tiles<D, 4, 1, 1>(a, p, BG, stream) : launch_tiles<D, 4, 1, 3>(a, p, BG, stream);
-    else bf16 ? launch_tiles<D, 2, 4, 1>(a, p, BG, stream) : launch_tiles<D, 2, 4, 3>(a, p, BG, stream);
+    else bf16 ? launch_tiles<D, 2, 2, 1>(a, p, BG, stream) : launch_tiles<D, 2, 2, 3>(a, p, BG, stream);
     return;
   }
   const dim3 grid(p.splits, (unsigned)p.tiles, (unsigned)BG);
