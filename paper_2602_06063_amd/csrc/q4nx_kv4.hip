@@ -291,6 +291,11 @@ struct AttnArgs {
 
 constexpr int kRowTile = 16, kAttnWaves = 4;
 
+// The running maximum is moved only when a score exceeds it by 2^kSlack: the
+// weights then reach 2^kSlack instead of 1, which rounds no differently, and
+// most blocks leave the outputs alone.
+constexpr float kSlack = 8.0f;
+
 // The blocks of 32 positions that a tile of rows attends to, and how many of
 // them a wave takes: shared by the two launches.
 struct TileRange {
@@ -375,6 +380,8 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
   const int64_t q_row = ((int64_t)b * a.T + t) * a.H + g * a.hg + (there ? row - t * a.hg : 0);
   const int pos = r.len - a.T + t;                                   // the row's own position
   const int row_hi = pos, row_lo = a.window ? pos - a.window + 1 : 0;
+  const int hi_min = r.len - a.T + r.t0, lo_max = a.window ? r.len - a.T + r.t1 - a.window + 1 : 0;  // what all rows see
+  const float scale2 = fabsf(a.scale2);
 
   // Q's operand: step s of lane group h covers the dims that K's words hold.
   u32x4 qf[NS];
@@ -382,6 +389,7 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
   for (int s = 0; s < NS; ++s) {
     const int dim = D == 64 ? 16 * h + 8 * s : (s / 4) * 128 + 32 * h + 8 * (s % 4);
     qf[s] = there ? *reinterpret_cast<const u32x4*>(a.q + q_row * D + dim) : (u32x4){0, 0, 0, 0};
+    if (a.scale2 < 0.0f) qf[s] ^= 0x80008000u;  // (the maximum is taken before the scale)
   }
 
   const uint8_t* kc = a.k + (int64_t)bg * a.P * (D / 2);
@@ -448,29 +456,37 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
       }
     }
     if (blk + 1 < w1) load_k(blk + 1);
-    // Running maximum, weights, correction.
-    float mx = m;
+    // Running maximum, correction, weights.
+    if (p0 < lo_max || p0 + kKvBlock - 1 > hi_min) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int p = p0 + 16 * i + 4 * h + e;
-        s[i][e] = p <= row_hi && p >= row_lo ? s[i][e] * a.scale2 : -INFINITY;
-        mx = fmaxf(mx, s[i][e]);
-      }
+        for (int e = 0; e < 4; ++e) {
+          const int p = p0 + 16 * i + 4 * h + e;
+          s[i][e] = p <= row_hi && p >= row_lo ? s[i][e] : -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e / 4][e % 4]);
     mx = fmaxf(mx, xor_lane<16>(mx));
-    mx = fmaxf(mx, xor_lane<32>(mx));
-    const float base = mx == -INFINITY ? 0.0f : mx;  // nothing seen yet: every weight is exp2(-inf) = 0
-    const float corr = __builtin_amdgcn_exp2f(m - base);
-    m = mx;
-    l *= corr;
+    mx = fmaxf(mx, xor_lane<32>(mx)) * scale2;
+    if (__ballot(mx > m + kSlack)) {
+      const float mn = fmaxf(m, mx);
+      const float corr = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+      m = mn;
+      l *= corr;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) y[i] *= corr;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;  // nothing seen yet: every weight is exp2(-inf) = 0
     u32x4 pf[NP];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       float f[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        f[e] = __builtin_amdgcn_exp2f(s[i][e] - base);
+        f[e] = __builtin_amdgcn_exp2f(fmaf(s[i][e], scale2, -base));
         l += f[e];
       }
 #pragma unroll
@@ -498,8 +514,6 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
           }
         }
     }
-#pragma unroll
-    for (int i = 0; i < NT; ++i) y[i] *= corr;
 #pragma unroll
     for (int u = 0; u < NG; ++u) {
       u32x4 lo, hi;
@@ -569,10 +583,10 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
   }
 }
 
-// Merges the splits of a row: grid (rows, row tiles -> flattened, D / 64) ...
-// workgroup (row of a group, B G, 64 values), 4 waves that take the splits in
-// turn; the sums run over a wave's splits in increasing order and then over
-// the waves.
+// Merges the splits of a row: workgroup (row of a group, B G, 64 values).  Each
+// of the 4 waves takes every fourth split, eight at a time (one round trip to
+// memory), with a running maximum; the waves' states are merged in order.
+constexpr int kMergeAhead = 8;
 template <int D>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(AttnArgs a, int tiles, int bf16) {
   __shared__ float ys[4][64], ls[4], ms[4];
@@ -584,31 +598,46 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(AttnArgs a, int tiles, i
   if (active <= 1) return;  // the first launch has written it
   const float* part = a.work + (((int64_t)bg * tiles + tile) * a.splits * kRowTile + row % kRowTile) * (D + 4);
   const int64_t step = (int64_t)kRowTile * (D + 4);
-  float m = -INFINITY;
-  for (int s = threadIdx.x; s < active; s += 256) m = fmaxf(m, part[s * step]);
-  m = fmaxf(m, xor_lane<1>(m));
-  m = fmaxf(m, xor_lane<2>(m));
-  m = fmaxf(m, xor_lane<4>(m));
-  m = fmaxf(m, xor_lane<8>(m));
-  m = fmaxf(m, xor_lane<16>(m));
-  m = fmaxf(m, xor_lane<32>(m));
-  if (lane == 0) ms[wave] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
-  const float base = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f, y = 0.0f;
-#pragma unroll 4
-  for (int s = wave; s < active; s += 4) {
-    const float c = __builtin_amdgcn_exp2f(part[s * step] - base);
-    l = fmaf(c, part[s * step + 1], l);
-    y = fmaf(c, part[s * step + 4 + dim], y);
+  float m = -INFINITY, l = 0.0f, y = 0.0f;
+  for (int s0 = wave; s0 < active; s0 += 4 * kMergeAhead) {
+    float pm[kMergeAhead], pl[kMergeAhead], py[kMergeAhead];
+#pragma unroll
+    for (int k = 0; k < kMergeAhead; ++k) {
+      const bool in = s0 + 4 * k < active;
+      const float* p = part + (in ? s0 + 4 * k : s0) * step;
+      pm[k] = in ? p[0] : -INFINITY;
+      pl[k] = p[1];
+      py[k] = p[4 + dim];
+    }
+    float mx = m;
+#pragma unroll
+    for (int k = 0; k < kMergeAhead; ++k) mx = fmaxf(mx, pm[k]);
+    const float base = mx == -INFINITY ? 0.0f : mx, c0 = __builtin_amdgcn_exp2f(m - base);
+    m = mx;
+    l *= c0;
+    y *= c0;
+#pragma unroll
+    for (int k = 0; k < kMergeAhead; ++k) {
+      const float c = __builtin_amdgcn_exp2f(pm[k] - base);  // 0 for a copy of s0's
+      l = fmaf(c, pl[k], l);
+      y = fmaf(c, py[k], y);
+    }
   }
   ys[wave][lane] = y;
-  if (lane == 0) ls[wave] = l;
+  if (lane == 0) {
+    ms[wave] = m;
+    ls[wave] = l;
+  }
   __syncthreads();
   if (wave == 0) {
-    const float lt = ls[0] + ls[1] + ls[2] + ls[3];
-    const float yt = ys[0][lane] + ys[1][lane] + ys[2][lane] + ys[3][lane];
+    const float mx = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3])), base = mx == -INFINITY ? 0.0f : mx;
+    float lt = 0.0f, yt = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float c = __builtin_amdgcn_exp2f(ms[w] - base);
+      lt = fmaf(c, ls[w], lt);
+      yt = fmaf(c, ys[w][lane], yt);
+    }
     const float o = lt == 0.0f ? 0.0f : yt / lt;
     const int t = row / a.hg;
     const int64_t i = (((int64_t)b * a.T + t) * a.H + g * a.hg + row - t * a.hg) * D + dim;
@@ -688,14 +717,37 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// One kilobyte from memory (a wave's own address, lane l's 16 bytes at 16 l,
-// which `lane16` holds) into LDS at byte `lds`.  As assembly, since the
-// compiler lets every later read of LDS wait for every such copy; the wait is
-// `arrived` below.  (It loads no registers; nothing else here uses M0, and the
-// idle step is what M0 needs before its use.)
-__device__ __forceinline__ void copy_lds(const u32x4* src, uint32_t lane16, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-               :: "v"(lane16), "s"(src), "s"(lds));
+// One kilobyte from memory (`offset`: the lane's 16 bytes from src) into LDS at
+// byte lds + kAt.  As assembly, since the compiler lets every later read of LDS
+// wait for every such copy; the wait is `arrived` below.  (It loads no
+// registers; nothing else here uses M0, and the idle step is what M0 needs
+// before its use.)
+template <int kAt>
+__device__ __forceinline__ void copy_lds(const u32x4* src, uint32_t offset, uint32_t lds) {
+  asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(offset), "s"(src), "s"(lds), "n"(kAt) : "scc");
+}
+
+template <int kStep, int N, int I = 0>
+__device__ __forceinline__ void copy_all(const u32x4* src, const uint32_t (&offset)[N], uint32_t lds) {
+  copy_lds<I * kStep>(src, offset[I], lds);
+  if constexpr (I + 1 < N) copy_all<kStep, N, I + 1>(src, offset, lds);
+}
+// Copy c of a batch, for a c known when the loop around it is unrolled.
+template <int kStep, int N>
+__device__ __forceinline__ void copy_one(const u32x4* src, const uint32_t (&offset)[N], uint32_t lds, int c) {
+  if (c == 0) copy_lds<0>(src, offset[0], lds);
+  if constexpr (N > 1) if (c == 1) copy_lds<kStep>(src, offset[1], lds);
+  if constexpr (N > 2) {
+    if (c == 2) copy_lds<2 * kStep>(src, offset[2], lds);
+    if (c == 3) copy_lds<3 * kStep>(src, offset[3], lds);
+  }
+  if constexpr (N > 4) {
+    if (c == 4) copy_lds<4 * kStep>(src, offset[4], lds);
+    if (c == 5) copy_lds<5 * kStep>(src, offset[5], lds);
+    if (c == 6) copy_lds<6 * kStep>(src, offset[6], lds);
+    if (c == 7) copy_lds<7 * kStep>(src, offset[7], lds);
+  }
 }
 
 // Attention of tiles of 32 RW rows (as in kv4_rows_kernel: S^T = K Q^T and
@@ -707,14 +759,9 @@ __device__ __forceinline__ void copy_lds(const u32x4* src, uint32_t lane16, uint
 // takes the exponentials of this one, so that the matrix unit works under the
 // vector unit's share of the step: K is a step ahead of V.
 //
-// The running maximum is moved only when a score exceeds it by 2^kSlack: the
-// weights then reach 2^kSlack instead of 1, which rounds no differently, and
-// most blocks leave the outputs alone.
 // grid: tiles with the longest ranges first, neighbours of one another on
 // different groups, so that each XCD (workgroups are dealt out to the 8 in
 // turn) works on few groups at a time.
-constexpr float kSlack = 8.0f;
-
 // Orders what stands between scheduling barriers: N times a matrix
 // instruction, V vector ones that run under it, a read of LDS and a copy into it
 // (copies in a row hold their wave up, 16 clocks each).
@@ -769,18 +816,24 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
   }
   const float scale2 = fabsf(a.scale2);
 
-  // In place of pieces past the last block, the last piece (every wave copies
-  // as often, so that it can wait for the older of two batches); positions past
-  // the rows' own are masked like all that a row does not see.
-  const int last = nblk * NC - 1;
-  const uint32_t buf_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)buf;
-  const auto copy_piece = [&](const u32x4* src, int which, int step, int i) __attribute__((always_inline)) {
-    copy_lds(src + (int64_t)min(step * KS * NC + W * i + wave, last) * 64, 16 * lane,
-             buf_lds + (((step & 1) * 2 + which) * (KS * kVec) + (W * i + wave) * 64) * 16);
+  // Steps past the last copy the last again (every wave copies as often, so that
+  // it can wait for all but the newest), and the last may copy a block past the
+  // tile's: its positions are masked like all that a row does not see.
+  const int steps = (nblk + KS - 1) / KS;
+  const uint32_t buf_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)buf + wave * 1024;
+  uint32_t offset[kCopies];
+#pragma unroll
+  for (int i = 0; i < kCopies; ++i) offset[i] = (W * i + wave) * 1024 + lane * 16;
+  struct Batch {
+    const u32x4* src;
+    uint32_t lds;
+  };
+  const auto batch = [&](const u32x4* src, int which, int step) __attribute__((always_inline)) {
+    return Batch{src + (int64_t)min(step, steps - 1) * (KS * kVec), buf_lds + ((step & 1) * 2 + which) * (KS * kVec * 16)};
   };
   const auto copy = [&](const u32x4* src, int which, int step) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i) copy_piece(src, which, step, i);
+    const Batch c = batch(src, which, step);
+    copy_all<W * 1024>(c.src, offset, c.lds);
   };
   // All but the newest two of the copies have arrived, and every wave has read
   // what it asked LDS for.  (A barrier of the language would wait for all.)
@@ -797,7 +850,6 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) y[i][e] = 0.0f;
-  const int steps = (nblk + KS - 1) / KS;
   u32x4 kf[NC];  // K's operands of the next step
   if (steps > 0) {
     copy(ksrc, 0, 0);
@@ -827,6 +879,7 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
     const u32x4* const k2 = operands(0, i + 2);
     const u32x4* const vb = operands(1, i);
     arrived();  // K of step i + 2
+    const Batch vc = batch(vsrc, 1, i + 1), kc = batch(ksrc, 0, i + 4);
     if (p0 < lo_max || p0 + kKvBlock - 1 > hi_min) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -843,7 +896,7 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
     for (int c = 0; c < NC / 2; ++c) {
       sn = mfma32(kf[c], qf[c], sn);
       kf[c] = k2[c * 64];
-      if (c < kCopies) copy_piece(vsrc, 1, i + 1, c);
+      if (c < kCopies) copy_one<W * 1024>(vc.src, offset, vc.lds, c);
     }
     float mx = s[0];
 #pragma unroll
@@ -903,7 +956,7 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
     for (int c = 0; c < 2 * NT; ++c) {
 #pragma unroll
       for (int u = 0; u < NP; ++u) y[c % NT] = mfma32(vf[c % kAhead], pf[u][c / NT], y[c % NT]);
-      if (c < kCopies) copy_piece(ksrc, 0, i + 4, c);
+      if (c < kCopies) copy_one<W * 1024>(kc.src, offset, kc.lds, c);
       const int r = c + kAhead;
       if (r < 2 * NT) vf[c % kAhead] = vb[(2 * (r % NT) + r / NT) * 64];
     }
@@ -994,14 +1047,14 @@ static AttnPlan attn_plan(int64_t B, int64_t T, int64_t H, int64_t G, int64_t L,
   return p;
 }
 static size_t attn_work_bytes(const AttnPlan& p, int64_t BG, int64_t d) {
-  if (p.rw) return (size_t)(BG * p.cap) * (size_t)(2 * kKvBlock * d * 2);
+  if (p.rw) return (size_t)(BG * p.cap + 1) * (size_t)(2 * kKvBlock * d * 2);  // (a step may copy a block past the last)
   return p.splits == 1 ? 0 : (size_t)(BG * p.tiles * p.splits * kRowTile * (d + 4)) * sizeof(float);
 }
 
 template <int D, int RW, int KS, int NP>
 static void launch_tiles(const AttnArgs& a, const AttnPlan& p, int64_t BG, hipStream_t stream) {
   u32x4* kx = reinterpret_cast<u32x4*>(a.work);
-  u32x4* vx = kx + BG * p.cap * (4 * D);
+  u32x4* vx = kx + (BG * p.cap + 1) * (4 * D);
   hipLaunchKernelGGL((kv4_tiles_kernel<D, RW, KS, NP>), dim3((unsigned)(BG * p.tiles)), dim3(64 * RW * KS), 0, stream, a,
                      kx, vx, (int)p.cap, (int)p.tiles, (int)BG);
 }
@@ -1012,7 +1065,7 @@ static void launch_attention(const AttnArgs& a, const AttnPlan& p, int64_t BG, b
     u32x4* kx = reinterpret_cast<u32x4*>(a.work);
     const int64_t x = std::min(p.cap, std::max<int64_t>(1, kExpandGroups / BG));
     hipLaunchKernelGGL((kv4_expand_kernel<D>), dim3((unsigned)x, (unsigned)BG), dim3(256), 0, stream, a, kx,
-                       kx + BG * p.cap * (4 * D), (int)p.cap);
+                       kx + (BG * p.cap + 1) * (4 * D), (int)p.cap);
     if (p.rw == 4) bf16 ? launch_tiles<D, 4, 1, 1>(a, p, BG, stream) : launch_tiles<D, 4, 1, 3>(a, p, BG, stream);
     else bf16 ? launch_tiles<D, 2, 2, 1>(a, p, BG, stream) : launch_tiles<D, 2, 2, 3>(a, p, BG, stream);
     return;
