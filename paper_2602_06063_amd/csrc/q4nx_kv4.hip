@@ -41,8 +41,9 @@ static inline int64_t kv_positions(int64_t L) { return ceil_div(L, kKvBlock) * k
 // ---------------------------------------------------------------------------
 // D / 8 lanes take a row of one head: lane j holds values 4j..4j+3 and
 // D/2 + 4j..+3, so that both values of a rotated pair are in one lane and a
-// group of 32 values is 8 lanes.  A wave takes 64 / (D / 8) heads at a time
-// (queries, then keys, then values of one token), `passes` times.
+// group of 32 values is 8 lanes.  A wave takes 64 / (D / 8) heads of a token
+// at a time, `passes` times, all queries or all keys or all values, so that
+// what they are is the wave's to know and not the lane's.
 struct StoreArgs {
   const void *q, *k, *v;
   const int32_t *positions, *seqs;
@@ -51,166 +52,257 @@ struct StoreArgs {
   uint16_t* q_out;
   uint8_t *k_cache, *v_cache;
   int64_t q_stride, k_stride, v_stride;
-  int64_t P;         // positions of a head in the cache: L, or whole blocks
-  int64_t heads_P;   // B G P
+  int64_t P;          // positions of a head in the cache: L, or whole blocks
+  int64_t heads_P;    // B G P
   int T, H, G, B, L;
-  int parts, passes; // waves of a token, and heads of a wave in steps of 64 / (D / 8)
+  int q_parts, kv_parts, passes;  // waves of a token's queries, and of its keys or values
   float weight_offset, eps;
 };
 
-// 4 consecutive values of a row.
+// 4 consecutive values of a row, as they are stored and as floats.
 template <bool F32>
-__device__ __forceinline__ f32x4 load4(const void* p, int64_t i) {
-  if constexpr (F32) {
-    return *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
-  } else {
-    const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
-    return (f32x4){bf16_to_f32(v.x & 0xFFFFu), __uint_as_float(v.x & 0xFFFF0000u), bf16_to_f32(v.y & 0xFFFFu),
-                   __uint_as_float(v.y & 0xFFFF0000u)};
-  }
+using Raw4 = std::conditional_t<F32, f32x4, uint2>;
+template <bool F32>
+__device__ __forceinline__ Raw4<F32> load4_raw(const void* p, int64_t i) {
+  if constexpr (F32) return *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
+  else return *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+}
+__device__ __forceinline__ f32x4 floats(f32x4 v) { return v; }
+__device__ __forceinline__ f32x4 floats(uint2 v) {
+  return (f32x4){bf16_to_f32(v.x & 0xFFFFu), __uint_as_float(v.x & 0xFFFF0000u), bf16_to_f32(v.y & 0xFFFFu),
+                 __uint_as_float(v.y & 0xFFFF0000u)};
 }
 
 __device__ __forceinline__ uint2 bf16x4_bits(f32x4 v) {
   return make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
 }
 
+// Lane l gets lane l ^ 7's value (the mirror of 8 lanes): once 4 neighbours hold
+// the same, an exchange with the other 4 in one instruction.
+__device__ __forceinline__ float other_quad(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x141, 0xF, 0xF, false));
+}
+
+// x / 15 rounded to nearest: a product and one correction (checked against the
+// division for every significand; a quotient below 2^-126 becomes 0 later), a
+// zero with its sign.
+__device__ __forceinline__ float div15(float x) {
+  constexpr float c = 1.0f / 15.0f;
+  const float q = x * c;
+  return copysignf(fmaf(fmaf(-15.0f, q, x), c, q), x);
+}
+
 // Codes (a byte each) and the (scale, offset) word of a group of 32 values, 4
-// to a lane in 8 consecutive lanes: the conversion of q4nx_quantize.
+// to a lane in 8 consecutive lanes: the conversion of q4nx_quantize, by its
+// rounded quotient t = v / d - m / d.  The bound e on the error of t and of the
+// levels (see quantize_kernel) is here u (128 + 2 R): the product m / d is
+// rounded on its own (u R), the rest as there.  What hardly ever occurs (values
+// to be clamped, NaN, a scale or offset below 2^-100, zero among them) is
+// looked for by the whole wave.
 __device__ __forceinline__ uint32_t group_codes(f32x4 v, uint32_t& pair) {
-  float lo = INFINITY, hi = -INFINITY;
+  const float top = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+  const float sum = v[0] + v[1] + v[2] + v[3];                      // a NaN shows here
+  if (__builtin_expect(__ballot(!(top <= kQuantClamp) || sum != sum) != 0, 0)) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    v[e] = v[e] != v[e] ? 0.0f : fminf(fmaxf(v[e], -kQuantClamp), kQuantClamp);
-    lo = fminf(lo, v[e]);
-    hi = fmaxf(hi, v[e]);
+    for (int e = 0; e < 4; ++e) v[e] = v[e] != v[e] ? 0.0f : fminf(fmaxf(v[e], -kQuantClamp), kQuantClamp);
   }
+  float lo = fminf(fminf(v[0], v[1]), fminf(v[2], v[3])), hi = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
   lo = fminf(lo, xor_lane<1>(lo));
   hi = fmaxf(hi, xor_lane<1>(hi));
   lo = fminf(lo, xor_lane<2>(lo));
   hi = fmaxf(hi, xor_lane<2>(hi));
-  lo = fminf(lo, xor_lane<4>(lo)) + 0.0f;  // a zero minimum is +0
-  hi = fmaxf(hi, xor_lane<4>(hi));
-  const uint32_t sb = bf16_rne_flushed((hi - lo) / 15.0f), mb = bf16_rne_flushed(lo);
-  pair = sb | (mb << 16);
-  const float d = bf16_to_f32(sb), m = bf16_to_f32(mb);
-  const float inv = d == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(d);  // d = 0: every code is 0
-  const float R = fabsf(m) * inv, near = 0.5f - kQuantU * (128.0f + R);
+  lo = fminf(lo, other_quad(lo)) + 0.0f;  // a zero minimum is +0
+  hi = fmaxf(hi, other_quad(hi));
+  pair = pack_bf16x2(div15(hi - lo), lo);
+  float d = bf16_to_f32(pair & 0xFFFFu), m = __uint_as_float(pair & 0xFFFF0000u);
+  float inv = __builtin_amdgcn_rcpf(d);
+  if (__builtin_expect(__ballot(!(fminf(fabsf(d), fabsf(m)) >= 0x1p-100f)) != 0, 0)) {
+    if (!(fabsf(d) >= 0x1p-100f)) {  // a signed zero, and every code 0
+      pair &= 0xFFFF8000u;
+      d = inv = 0.0f;
+    }
+    if (!(fabsf(m) >= 0x1p-100f)) {
+      pair &= 0x8000FFFFu;
+      m = 0.0f;
+    }
+  }
+  const float shift = m * inv, R = fabsf(shift), near = 0.5f - kQuantU * (128.0f + 2.0f * R);
   uint32_t codes = 0;
+  float x[4], c[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float x = (v[e] - m) * inv, c = rintf(x);
-    uint32_t q = (uint32_t)__builtin_amdgcn_fmed3f(c, 0.0f, 15.0f);
-    if (!(R <= kQuantMaxR && fabsf(x - c) <= near)) q = (uint32_t)quant_code(v[e], d, m);
-    codes |= q << (8 * e);
+    x[e] = fmaf(v[e], inv, -shift);
+    c[e] = rintf(x[e]);
+    x[e] -= c[e];
+    codes = __builtin_amdgcn_cvt_pk_u8_f32(__builtin_amdgcn_fmed3f(c[e], 0.0f, 15.0f), e, codes);
+  }
+  const float off = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
+  if (!(R <= kQuantMaxR && off <= near)) {
+    codes = 0;
+#pragma unroll 1
+    for (int e = 0; e < 4; ++e) codes |= (uint32_t)quant_code(e == 0 ? v[0] : e == 1 ? v[1] : e == 2 ? v[2] : v[3], d, m) << (8 * e);
   }
   return codes;
 }
 
+// Workgroups are dealt out to the 8 XCDs in turn; this gives each XCD a run of
+// neighbouring ones, so that the bytes of a V block, which neighbouring tokens
+// share, meet in one L2.  The grid is a multiple of 8.
+constexpr int kXcds = 8;
+__device__ __forceinline__ int64_t xcd_run(int64_t block, int64_t grid) {
+  return block % kXcds * (grid / kXcds) + block / kXcds;
+}
+
 template <int D, bool F32, bool Q4>
 __global__ __launch_bounds__(256) void kv_store_kernel(StoreArgs a) {
-  constexpr int R = D / 8, RW = 64 / R;
+  constexpr int R = D / 8, RW = 64 / R, kAhead = 4;
   const int lane = threadIdx.x & 63, j = lane % R, sub = lane / R;
-  const int64_t wid = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t t = wid / a.parts;
+  const uint32_t wid = (uint32_t)xcd_run(blockIdx.x, gridDim.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t parts = a.q_parts + 2 * a.kv_parts;
+  const int t = __builtin_amdgcn_readfirstlane(wid / parts);
   if (t >= a.T) return;
-  const int part = (int)(wid - t * a.parts);
+  int part = (int)(wid - t * parts);
+  const int kind = part < a.q_parts ? 0 : part < a.q_parts + a.kv_parts ? 1 : 2;  // queries, keys, values
+  part -= kind == 0 ? 0 : kind == 1 ? a.q_parts : a.q_parts + a.kv_parts;
+  const int heads = kind == 0 ? a.H : a.G;
+  const int h0 = part * a.passes * RW;
+  const int passes = min(a.passes, (heads - h0 + RW - 1) / RW);
+  const char* const row = static_cast<const char*>(kind == 0 ? a.q : kind == 1 ? a.k : a.v) +
+                          t * (kind == 0 ? a.q_stride : kind == 1 ? a.k_stride : a.v_stride) * (F32 ? 4 : 2);
+  // The values of kAhead steps are requested at once, the first before the
+  // position is known (which says whether there is anything to do).  Lanes past
+  // the last head work on the last once more and store nothing.
+  Raw4<F32> rx[kAhead], ry[kAhead];
+  const auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (i == 0 || s0 + i < passes) {
+        const int at = min(h0 + (s0 + i) * RW + sub, heads - 1) * D + 4 * j;
+        rx[i] = load4_raw<F32>(row, at);
+        ry[i] = load4_raw<F32>(row, at + D / 2);
+      }
+  };
+  load(0);
   const int pos = a.positions[t];
   const int seq = a.seqs ? a.seqs[t] : 0;
   if (pos < 0 || pos >= a.L || seq < 0 || seq >= a.B) return;  // the whole wave: a padded token
 
-  const int e0 = part * a.passes * RW;
-  const int heads = a.H + 2 * a.G;
+  // out_i = r (x_i A - x_(i+d/2) B), out_(i+d/2) = r (x_(i+d/2) C + x_i E), with
+  // the weights and the angle's cosine and sine in A = w_i cos, B = w_(i+d/2) sin,
+  // C = w_(i+d/2) cos, E = w_i sin and the head's 1 / sqrt(mean + eps) in r.
   // The angle of pair i is pos * inv_freq[i], an exact product in 64 bits,
   // whole turns taken off before it becomes float32: at position 10^5 a
   // float32 angle is off by 2^-8 radians.  The turn's sine and cosine are
   // good to some 2^-20, far below the 2^-9 of a stored value.
-  f32x4 cs = {1.0f, 1.0f, 1.0f, 1.0f}, sn = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (a.inv_freq && e0 < a.H + a.G) {
-    const f32x4 f = *reinterpret_cast<const f32x4*>(a.inv_freq + 4 * j);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const double turns = (double)pos * (double)f[e] * 0.15915494309189535;
-      const float frac = (float)(turns - rint(turns));
-      sn[e] = __builtin_amdgcn_sinf(frac);
-      cs[e] = __builtin_amdgcn_cosf(frac);
-    }
-  }
-#pragma unroll 1
-  for (int s = 0; s < a.passes; ++s) {
-    const int h = e0 + s * RW + sub;
-    if (e0 + s * RW >= heads) break;
-    const bool is_q = h < a.H, is_k = !is_q && h < a.H + a.G, there = h < heads;
-    const int hk = is_q ? h : is_k ? h - a.H : there ? h - a.H - a.G : a.G - 1;
-    const void* src = is_q ? a.q : is_k ? a.k : a.v;
-    const int64_t at = t * (is_q ? a.q_stride : is_k ? a.k_stride : a.v_stride) + (int64_t)hk * D + 4 * j;
-    f32x4 x = load4<F32>(src, at), y = load4<F32>(src, at + D / 2);
-    const uint16_t* w = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
-    // Every lane takes part in the lane exchanges; values keep what they are.
-    float ss = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
-    ss += xor_lane<1>(ss);
-    ss += xor_lane<2>(ss);
-    ss += xor_lane<4>(ss);
-    if constexpr (R >= 16) ss += xor_lane<8>(ss);
-    if constexpr (R >= 32) ss += xor_lane<16>(ss);
+  const uint16_t* const w = kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr;
+  const bool turn = a.inv_freq && kind < 2;
+  f32x4 A, B, C, E;
+  {
+    f32x4 wx = {1.0f, 1.0f, 1.0f, 1.0f}, wy = wx;
     if (w) {
-      const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
-      const f32x4 wx = load4<false>(w, 4 * j), wy = load4<false>(w, D / 2 + 4 * j);
+      wx = floats(load4_raw<false>(w, 4 * j)) + a.weight_offset;
+      wy = floats(load4_raw<false>(w, D / 2 + 4 * j)) + a.weight_offset;
+    }
+    A = wx;
+    C = wy;
+    if (turn) {
+      const f32x4 f = *reinterpret_cast<const f32x4*>(a.inv_freq + 4 * j);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[e] = x[e] * r * (a.weight_offset + wx[e]);
-        y[e] = y[e] * r * (a.weight_offset + wy[e]);
+        const double turns = (double)pos * (double)f[e] * 0.15915494309189535;
+        const float frac = (float)(turns - rint(turns));
+        const float sn = __builtin_amdgcn_sinf(frac), cs = __builtin_amdgcn_cosf(frac);
+        A[e] = wx[e] * cs;
+        B[e] = wy[e] * sn;
+        C[e] = wy[e] * cs;
+        E[e] = wx[e] * sn;
       }
     }
-    if (a.inv_freq && (is_q || is_k)) {  // (an infinite value times a sine of 0 would be NaN)
+  }
+
+  const int blk = pos >> 5, pa = (pos >> 4) & 1, ph = (pos >> 2) & 3, pr = pos & 3;
+  const auto step = [&](int s, f32x4 x, f32x4 y) __attribute__((always_inline)) {
+    const int h = h0 + s * RW + sub;
+    const bool there = h < heads;
+    if (w) {
+      float ss = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
+      ss += xor_lane<1>(ss);
+      ss += xor_lane<2>(ss);
+      ss += other_quad(ss);
+      if constexpr (R >= 16) ss += xor_lane<8>(ss);
+      if constexpr (R >= 32) ss += xor_lane<16>(ss);
+      // (The instruction takes a subnormal for 0.)
+      const float mean = ss * (1.0f / D) + a.eps;
+      const float r = mean < 0x1p-100f ? __builtin_amdgcn_rsqf(mean * 0x1p64f) * 0x1p32f : __builtin_amdgcn_rsqf(mean);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float lo = x[e] * cs[e] - y[e] * sn[e], hi = y[e] * cs[e] + x[e] * sn[e];
+        x[e] *= r;
+        y[e] *= r;
+      }
+    }
+    if (turn) {  // (without a turn, an infinite value times a sine of 0 would be NaN)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float lo = x[e] * A[e] - y[e] * B[e], hi = y[e] * C[e] + x[e] * E[e];
         x[e] = lo;
         y[e] = hi;
       }
+    } else if (w) {
+      x *= A;
+      y *= C;
     }
-    if (is_q) {
-      uint16_t* o = a.q_out + (t * a.H + h) * D + 4 * j;
-      *reinterpret_cast<uint2*>(o) = bf16x4_bits(x);
-      *reinterpret_cast<uint2*>(o + D / 2) = bf16x4_bits(y);
+    if (kind == 0) {
+      if (there) {
+        uint16_t* const o = a.q_out + ((int64_t)t * a.H + h) * D + 4 * j;
+        *reinterpret_cast<uint2*>(o) = bf16x4_bits(x);
+        *reinterpret_cast<uint2*>(o + D / 2) = bf16x4_bits(y);
+      }
+      return;
     }
-    const int64_t head = (int64_t)seq * a.G + hk;
+    const int64_t head = (int64_t)seq * a.G + min(h, heads - 1);
+    uint8_t* const cache = kind == 1 ? a.k_cache : a.v_cache;
     if constexpr (!Q4) {
-      if (there && !is_q) {
-        uint16_t* o = reinterpret_cast<uint16_t*>(is_k ? a.k_cache : a.v_cache) + (head * a.P + pos) * D + 4 * j;
+      if (there) {
+        uint16_t* const o = reinterpret_cast<uint16_t*>(cache) + (head * a.P + pos) * D + 4 * j;
         *reinterpret_cast<uint2*>(o) = bf16x4_bits(x);
         *reinterpret_cast<uint2*>(o + D / 2) = bf16x4_bits(y);
       }
     } else {
-      if (e0 + s * RW + RW <= a.H) continue;  // the whole wave: only queries
       uint32_t pair[2], code[2] = {group_codes(x, pair[0]), group_codes(y, pair[1])};
       const int u = j & 7, g0 = j >> 3;  // groups g0 and g0 + D / 64
+      uint32_t* const pairs = reinterpret_cast<uint32_t*>(cache + a.heads_P * (D / 2)) + head * a.P * (D / 32);
+      uint8_t* const codes = cache + head * a.P * (D / 2);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int g = g0 + i * (D / 64);
-        const uint32_t odd = (uint32_t)xor_lane_bits<1>((int)code[i]), far = (uint32_t)xor_lane_bits<4>((int)code[i]);
-        if (is_k) {
-          if ((u & 1) == 0)
-            *reinterpret_cast<uint32_t*>(a.k_cache + (head * a.P + pos) * (D / 2) + 16 * g + 2 * u) = code[i] | (odd << 4);
-          if (u == 0)
-            reinterpret_cast<uint32_t*>(a.k_cache + a.heads_P * (D / 2))[(head * a.P + pos) * (D / 32) + g] = pair[i];
-        } else if (there && !is_q) {
-          const int blk = pos >> 5, pa = (pos >> 4) & 1, ph = (pos >> 2) & 3, pr = pos & 3;
-          if (u < 4) {
-            const uint32_t both = code[i] | (far << 4);
-            uint8_t* o = a.v_cache + head * a.P * (D / 2) + (int64_t)blk * (16 * D) + (g >> 1) * 1024 +
-                         (ph * 16 + 4 * u) * 16 + (g & 1) * 8 + pa * 4 + pr;
+        if (kind == 1) {
+          const uint32_t odd = (uint32_t)xor_lane_bits<1>((int)code[i]);
+          if (there && (u & 1) == 0)
+            *reinterpret_cast<uint32_t*>(codes + (int64_t)pos * (D / 2) + 16 * g + 2 * u) = code[i] | (odd << 4);
+          if (there && u == 0) pairs[(int64_t)pos * (D / 32) + g] = pair[i];
+        } else {
+          const uint32_t both = code[i] | ((uint32_t)xor_lane_bits<4>((int)code[i]) << 4);
+          if (there && u < 4) {
+            uint8_t* const o = codes + (int64_t)blk * (16 * D) + (g >> 1) * 1024 + (ph * 16 + 4 * u) * 16 + (g & 1) * 8 +
+                               pa * 4 + pr;
 #pragma unroll
             for (int b = 0; b < 4; ++b) o[16 * b] = (uint8_t)(both >> (8 * b));
           }
-          if (u == 0)
-            reinterpret_cast<uint32_t*>(a.v_cache + a.heads_P * (D / 2))[head * a.P * (D / 32) + (int64_t)blk * D +
-                                                                         g * 32 + ph * 8 + pa * 4 + pr] = pair[i];
+          if (there && u == 0) pairs[(int64_t)blk * D + g * 32 + ph * 8 + pa * 4 + pr] = pair[i];
         }
       }
     }
+  };
+#pragma unroll 1
+  for (int s0 = 0;;) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (i == 0 || s0 + i < passes) step(s0 + i, floats(rx[i]), floats(ry[i]));
+    s0 += kAhead;
+    if (s0 >= passes) break;
+    load(s0);
   }
 }
 
@@ -246,7 +338,7 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(const uint8_t* __restrict
                                                        void* __restrict__ v_out, int T, int G, int B, int L, int64_t P,
                                                        int64_t heads_P) {
   constexpr int R = D / 8;
-  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / R;
+  const int64_t row = (xcd_run(blockIdx.x, gridDim.x) * 256 + threadIdx.x) / R;
   const int j = threadIdx.x % R;
   if (row >= (int64_t)T * G) return;
   const int64_t t = row / G;
@@ -287,7 +379,13 @@ struct AttnArgs {
   int T, H, G, L, window, rows;  // rows = T H / G of a KV group
   int hg, splits;
   float scale2;                  // scale * log2(e)
+  uint32_t by_hg, by_G, by_waves;  // reciprocals of hg, G and the waves of all splits (see over)
 };
+
+// x / n by a multiplication with 2^32 / n rounded up (0 for n = 1): exact for
+// x n < 2^32, and above that at most too large, never too small.
+static uint32_t reciprocal(int64_t n) { return n == 1 ? 0u : (uint32_t)(((int64_t(1) << 32) + n - 1) / n); }
+__device__ __forceinline__ int over(int x, uint32_t by) { return by ? (int)__umulhi((uint32_t)x, by) : x; }
 
 constexpr int kRowTile = 16, kAttnWaves = 4;
 
@@ -305,18 +403,17 @@ struct TileRange {
 __device__ __forceinline__ TileRange tile_range(const AttnArgs& a, int b, int tile) {
   TileRange r;
   r.len = min(max(a.lens[b], 0), a.L);
-  r.t0 = tile * kRowTile / a.hg;
-  r.t1 = min(a.T - 1, (tile * kRowTile + kRowTile - 1) / a.hg);
+  r.t0 = over(tile * kRowTile, a.by_hg);
+  r.t1 = min(a.T - 1, over(tile * kRowTile + kRowTile - 1, a.by_hg));
   r.j1 = max(0, r.len - a.T + r.t1 + 1);
   r.j0 = a.window ? max(0, max(0, r.len - a.T + r.t0) - a.window + 1) : 0;
   r.blk0 = r.j0 / kKvBlock;
   r.nblk = r.j1 > r.j0 ? (r.j1 + kKvBlock - 1) / kKvBlock - r.blk0 : 0;
-  const int nw = a.splits * kAttnWaves;
-  r.per = max(1, (r.nblk + nw - 1) / nw);
+  r.per = max(1, over(r.nblk + a.splits * kAttnWaves - 1, a.by_waves));
   return r;
 }
 __device__ __forceinline__ int active_splits(const TileRange& r) {
-  return (r.nblk + r.per * kAttnWaves - 1) / (r.per * kAttnWaves);
+  return r.nblk <= r.per * kAttnWaves ? 1 : (r.nblk + r.per * kAttnWaves - 1) / (r.per * kAttnWaves);
 }
 
 __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
@@ -369,14 +466,14 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
   __shared__ float ms[kAttnWaves][kRowTile], ls[kAttnWaves][kRowTile];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, h = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int split = blockIdx.x, tile = blockIdx.y, bg = blockIdx.z, b = bg / a.G, g = bg - b * a.G;
+  const int split = blockIdx.x, tile = blockIdx.y, bg = blockIdx.z, b = over(bg, a.by_G), g = bg - b * a.G;
   const TileRange r = tile_range(a, b, tile);
   const int active = active_splits(r);
   if (split >= max(active, 1)) return;  // the whole workgroup
 
   const int row = tile * kRowTile + n;
   const bool there = row < a.rows;
-  const int t = there ? row / a.hg : r.t1;
+  const int t = there ? over(row, a.by_hg) : r.t1;
   const int64_t q_row = ((int64_t)b * a.T + t) * a.H + g * a.hg + (there ? row - t * a.hg : 0);
   const int pos = r.len - a.T + t;                                   // the row's own position
   const int row_hi = pos, row_lo = a.window ? pos - a.window + 1 : 0;
@@ -568,10 +665,10 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
       yt += c * *reinterpret_cast<const f32x4*>(&ys[w][rr][dd]);
     }
     if (active <= 1) {
-      const int R = tile * kRowTile + rr, tt = R / a.hg;
+      const int R = tile * kRowTile + rr, tt = over(R, a.by_hg);
       const int64_t o = (((int64_t)b * a.T + tt) * a.H + g * a.hg + R - tt * a.hg) * D + dd;
       // A row that attends to nothing is zero.
-      put4(a.o, NP == 2, o, lt == 0.0f ? (f32x4){0.0f, 0.0f, 0.0f, 0.0f} : yt / lt);
+      put4(a.o, NP < 3, o, lt == 0.0f ? (f32x4){0.0f, 0.0f, 0.0f, 0.0f} : yt / lt);
     } else {
       float* part = a.work + ((((int64_t)bg * gridDim.y + tile) * a.splits + split) * kRowTile + rr) * (D + 4);
       *reinterpret_cast<f32x4*>(part + 4 + dd) = yt;
@@ -584,13 +681,13 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
 }
 
 // Merges the splits of a row: workgroup (row of a group, B G, 64 values).  Each
-// of the 4 waves takes every fourth split, eight at a time (one round trip to
+// of the 8 waves takes every eighth split, eight at a time (one round trip to
 // memory), with a running maximum; the waves' states are merged in order.
-constexpr int kMergeAhead = 8;
+constexpr int kMergeAhead = 8, kMergeWaves = 8;
 template <int D>
-__global__ __launch_bounds__(256) void kv4_merge_kernel(AttnArgs a, int tiles, int bf16) {
-  __shared__ float ys[4][64], ls[4], ms[4];
-  const int row = blockIdx.x, bg = blockIdx.y, b = bg / a.G, g = bg - b * a.G;
+__global__ __launch_bounds__(64 * kMergeWaves) void kv4_merge_kernel(AttnArgs a, int tiles, int bf16) {
+  __shared__ float ys[kMergeWaves][64], ls[kMergeWaves], ms[kMergeWaves];
+  const int row = blockIdx.x, bg = blockIdx.y, b = over(bg, a.by_G), g = bg - b * a.G;
   const int tile = row / kRowTile;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, dim = blockIdx.z * 64 + lane;
   const TileRange r = tile_range(a, b, tile);
@@ -599,12 +696,12 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(AttnArgs a, int tiles, i
   const float* part = a.work + (((int64_t)bg * tiles + tile) * a.splits * kRowTile + row % kRowTile) * (D + 4);
   const int64_t step = (int64_t)kRowTile * (D + 4);
   float m = -INFINITY, l = 0.0f, y = 0.0f;
-  for (int s0 = wave; s0 < active; s0 += 4 * kMergeAhead) {
+  for (int s0 = wave; s0 < active; s0 += kMergeWaves * kMergeAhead) {
     float pm[kMergeAhead], pl[kMergeAhead], py[kMergeAhead];
 #pragma unroll
     for (int k = 0; k < kMergeAhead; ++k) {
-      const bool in = s0 + 4 * k < active;
-      const float* p = part + (in ? s0 + 4 * k : s0) * step;
+      const bool in = s0 + kMergeWaves * k < active;
+      const float* p = part + (in ? s0 + kMergeWaves * k : s0) * step;
       pm[k] = in ? p[0] : -INFINITY;
       pl[k] = p[1];
       py[k] = p[4 + dim];
@@ -630,16 +727,19 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(AttnArgs a, int tiles, i
   }
   __syncthreads();
   if (wave == 0) {
-    const float mx = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3])), base = mx == -INFINITY ? 0.0f : mx;
+    float mx = ms[0];
+#pragma unroll
+    for (int w = 1; w < kMergeWaves; ++w) mx = fmaxf(mx, ms[w]);
+    const float base = mx == -INFINITY ? 0.0f : mx;
     float lt = 0.0f, yt = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < kMergeWaves; ++w) {
       const float c = __builtin_amdgcn_exp2f(ms[w] - base);
       lt = fmaf(c, ls[w], lt);
       yt = fmaf(c, ys[w][lane], yt);
     }
     const float o = lt == 0.0f ? 0.0f : yt / lt;
-    const int t = row / a.hg;
+    const int t = over(row, a.by_hg);
     const int64_t i = (((int64_t)b * a.T + t) * a.H + g * a.hg + row - t * a.hg) * D + dim;
     if (bf16) static_cast<uint16_t*>(a.o)[i] = f32_to_bf16_bits(o);
     else static_cast<float*>(a.o)[i] = o;
@@ -666,7 +766,7 @@ __device__ __forceinline__ int first_block(const AttnArgs& a, int len) {
 template <int D>
 __global__ __launch_bounds__(256) void kv4_expand_kernel(AttnArgs a, u32x4* __restrict__ ko, u32x4* __restrict__ vo,
                                                          int cap) {
-  const int bg = blockIdx.y, b = bg / a.G;
+  const int bg = blockIdx.y, b = over(bg, a.by_G);
   const int len = min(max(a.lens[b], 0), a.L);
   const int base = first_block(a, len), nblk = (len + kKvBlock - 1) / kKvBlock - base;
   const int j0 = a.window ? max(0, max(0, len - a.T) - a.window + 1) : 0;
@@ -789,20 +889,20 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
   __shared__ float ms[KS][kRows], ls[KS][kRows];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, ks = wave / RW;
-  const int bg = blockIdx.x % BG, tile = tiles - 1 - blockIdx.x / BG, b = bg / a.G, g = bg - b * a.G;
+  const int bg = blockIdx.x % BG, tile = tiles - 1 - blockIdx.x / BG, b = over(bg, a.by_G), g = bg - b * a.G;
   const int len = __builtin_amdgcn_readfirstlane(min(max(a.lens[b], 0), a.L)), first = len - a.T;  // position of row 0
 
   const int r0 = tile * kRows + 32 * rw;
   const int row = r0 + n;
   const bool there = row < a.rows;
-  const int t = there ? row / a.hg : a.T - 1;
+  const int t = there ? over(row, a.by_hg) : a.T - 1;
   const int64_t q_row = ((int64_t)b * a.T + t) * a.H + g * a.hg + (there ? row - t * a.hg : 0);
   const int row_hi = first + t, row_lo = a.window ? row_hi - a.window + 1 : 0;
   // Positions of the workgroup's rows, and what all the wave's rows see.
-  const int wg_hi = __builtin_amdgcn_readfirstlane(first + min(a.T - 1, (tile * kRows + kRows - 1) / a.hg));
-  const int wg_lo = __builtin_amdgcn_readfirstlane(a.window ? max(0, max(0, first + tile * kRows / a.hg) - a.window + 1) : 0);
-  const int hi_min = __builtin_amdgcn_readfirstlane(first + min(r0 / a.hg, a.T - 1));
-  const int lo_max = __builtin_amdgcn_readfirstlane(a.window ? first + min(a.T - 1, (r0 + 31) / a.hg) - a.window + 1 : 0);
+  const int wg_hi = __builtin_amdgcn_readfirstlane(first + min(a.T - 1, over(tile * kRows + kRows - 1, a.by_hg)));
+  const int wg_lo = __builtin_amdgcn_readfirstlane(a.window ? max(0, max(0, first + over(tile * kRows, a.by_hg)) - a.window + 1) : 0);
+  const int hi_min = __builtin_amdgcn_readfirstlane(first + min(over(r0, a.by_hg), a.T - 1));
+  const int lo_max = __builtin_amdgcn_readfirstlane(a.window ? first + min(a.T - 1, over(r0 + 31, a.by_hg)) - a.window + 1 : 0);
   const int base = __builtin_amdgcn_readfirstlane(first_block(a, len));
   const int blk0 = wg_lo / kKvBlock, nblk = wg_hi >= wg_lo ? wg_hi / kKvBlock + 1 - blk0 : 0;
   const u32x4* ksrc = kx + ((int64_t)bg * cap + blk0 - base) * kVec;
@@ -1012,7 +1112,7 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
     for (int k = 0; k < NT; ++k)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        put4(a.o, NP == 1, q_row * D + 32 * k + 8 * e + 4 * half,
+        put4(a.o, NP < 3, q_row * D + 32 * k + 8 * e + 4 * half,
              (f32x4){y[k][4 * e] * inv, y[k][4 * e + 1] * inv, y[k][4 * e + 2] * inv, y[k][4 * e + 3] * inv});
   }
 }
@@ -1074,25 +1174,28 @@ static void launch_attention(const AttnArgs& a, const AttnPlan& p, int64_t BG, b
   if (bf16) hipLaunchKernelGGL((kv4_rows_kernel<D, 2>), grid, dim3(64 * kAttnWaves), 0, stream, a);
   else hipLaunchKernelGGL((kv4_rows_kernel<D, 3>), grid, dim3(64 * kAttnWaves), 0, stream, a);
   if (p.splits > 1)
-    hipLaunchKernelGGL((kv4_merge_kernel<D>), dim3((unsigned)p.rows, (unsigned)BG, D / 64), dim3(256), 0, stream, a,
+    hipLaunchKernelGGL((kv4_merge_kernel<D>), dim3((unsigned)p.rows, (unsigned)BG, D / 64), dim3(64 * kMergeWaves), 0,
+                       stream, a,
                        (int)p.tiles, (int)bf16);
 }
 
 // ---- launchers ------------------------------------------------------------
+constexpr int64_t kStoreWaves = 16384;
 template <int D, bool F32, bool Q4>
 static void launch_store(const StoreArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((kv_store_kernel<D, F32, Q4>), dim3((unsigned)ceil_div((int64_t)a.T * a.parts, 4)), dim3(256), 0,
-                     stream, a);
+  const int64_t groups = ceil_div((int64_t)a.T * (a.q_parts + 2 * a.kv_parts), 4 * kXcds) * kXcds;
+  hipLaunchKernelGGL((kv_store_kernel<D, F32, Q4>), dim3((unsigned)groups), dim3(256), 0, stream, a);
 }
 
 template <int D>
 static void dispatch_store(StoreArgs a, bool f32, bool q4, hipStream_t stream) {
   constexpr int RW = 512 / D;
-  const int64_t steps = ceil_div(a.H + 2 * (int64_t)a.G, RW);
-  // A wave per head group while there are few of them, and whole tokens (the
-  // angles taken once) where there are many.
-  a.passes = (int)std::max<int64_t>(1, std::min(steps, a.T * steps / 8192));
-  a.parts = (int)ceil_div(steps, a.passes);
+  const int64_t q_steps = ceil_div(a.H, RW), kv_steps = ceil_div(a.G, RW);
+  // A wave per head group while there are few of them; where there are many,
+  // longer ones (a wave's angles and weights are taken once).
+  a.passes = (int)std::max<int64_t>(1, std::min(std::max(q_steps, kv_steps), a.T * (q_steps + 2 * kv_steps) / kStoreWaves));
+  a.q_parts = (int)ceil_div(q_steps, a.passes);
+  a.kv_parts = (int)ceil_div(kv_steps, a.passes);
   if (f32 && q4) launch_store<D, true, true>(a, stream);
   else if (f32) launch_store<D, true, false>(a, stream);
   else if (q4) launch_store<D, false, true>(a, stream);
@@ -1195,7 +1298,7 @@ q4nx_status q4nx_kv4_load(const void* d_k, const void* d_v, const int32_t* d_pos
     return fail(Q4NX_ERR_ALIGNMENT, f + ": caches and outputs need 16-byte alignment, positions and seqs 4-byte");
   if (T * G > (int64_t(1) << 32)) return fail(Q4NX_ERR_SHAPE, f + ": T G must not exceed 2^32");
   const int64_t P = kv_positions(L);
-  const dim3 grid((unsigned)ceil_div(T * G * (d / 8), 256));
+  const dim3 grid((unsigned)(ceil_div(T * G * (d / 8), 256 * kXcds) * kXcds));
   const auto go = [&](auto dc, auto fc) {
     hipLaunchKernelGGL((kv4_load_kernel<decltype(dc)::value, decltype(fc)::value>), grid, dim3(256), 0, stream,
                        static_cast<const uint8_t*>(d_k), static_cast<const uint8_t*>(d_v), d_positions, d_seqs, d_k_out,
@@ -1261,6 +1364,9 @@ q4nx_status q4nx_kv4_attention(const uint16_t* d_q, const void* d_k, const void*
   a.rows = (int)p.rows;
   a.hg = (int)(H / G);
   a.splits = p.splits;
+  a.by_hg = reciprocal(H / G);
+  a.by_G = reciprocal(G);
+  a.by_waves = reciprocal((int64_t)p.splits * kAttnWaves);
   // A scale of zero (equal weights) becomes the smallest normal one, which
   // leaves any finite score below 2^-25 but a masked one at -inf.
   a.scale2 = scale * 1.4426950408889634f;
