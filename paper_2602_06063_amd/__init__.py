@@ -435,6 +435,17 @@ def _cache_bytes(B: int, G: int, d: int, L: int, kv_format: int) -> int:
     return B * G * ((L + 31) >> 5) * 20 * d if kv_format == Q4NX_KV_Q4 else 2 * B * G * L * d
 
 
+def _ptr(t, nbytes: int, what: str) -> int:
+    """_need and _dptr in one (these calls are as short as their launches)."""
+    if not t.is_cuda:
+        raise ValueError("expected a GPU tensor")
+    if not t.is_contiguous():
+        raise ValueError("expected a contiguous tensor")
+    if t.nbytes < nbytes:
+        raise ValueError(f"{what}: {t.nbytes} bytes, need {nbytes}")
+    return t.data_ptr()
+
+
 def _rows(t, T: int, width: int, what: str):
     """Pointer and row stride (elements) of T rows of `width` values: a contiguous tensor, or a view of whole rows
     of a wider one, as a stacked projection's columns are."""
@@ -444,16 +455,16 @@ def _rows(t, T: int, width: int, what: str):
         if t.numel() < T * width:
             raise ValueError(f"{what}: {t.numel()} elements, need {T * width}")
         return t.data_ptr(), width
-    if t.dim() != 2 or t.stride(1) != 1 or t.shape[0] < T or t.shape[1] < width:
+    stride, shape = t.stride(), t.shape
+    if len(shape) != 2 or stride[1] != 1 or shape[0] < T or shape[1] < width:
         raise ValueError(f"{what}: expected a contiguous tensor, or 2-d rows of at least {width} contiguous values")
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), stride[0]
 
 
 def _ints(t, n: int, what: str) -> int:
     if t.dtype != _torch.int32:
         raise ValueError(f"{what}: expected int32")
-    _need(t, 4 * n, what)
-    return _dptr(t)
+    return _ptr(t, 4 * n, what)
 
 
 def q4nx_kv_store(q, k, v, positions, q_out, k_cache, v_cache, T: int, H: int, G: int, d: int, B: int, L: int,
@@ -466,28 +477,19 @@ def q4nx_kv_store(q, k, v, positions, q_out, k_cache, v_cache, T: int, H: int, G
     qp, qs = _rows(q, T, H * d, "q")
     kp, ks = _rows(k, T, G * d, "k")
     vp, vs = _rows(v, T, G * d, "v")
-    if k.dtype != q.dtype or v.dtype != q.dtype:
+    dtype = q.dtype
+    if k.dtype != dtype or v.dtype != dtype:
         raise ValueError("q, k and v must share one dtype")
+    if inv_freq is not None and inv_freq.dtype != _F32:
+        raise ValueError("inv_freq: expected float32")
     cache = _cache_bytes(B, G, d, L, kv_format)
-    _need(q_out, 2 * T * H * d, "q_out")
-    _need(k_cache, cache, "k_cache")
-    _need(v_cache, cache, "v_cache")
-    qw = kw = fr = sq = 0
-    if q_weight is not None:
-        _need(q_weight, 2 * d, "q_weight")
-        qw = _dptr(q_weight)
-    if k_weight is not None:
-        _need(k_weight, 2 * d, "k_weight")
-        kw = _dptr(k_weight)
-    if inv_freq is not None:
-        if inv_freq.dtype != _F32:
-            raise ValueError("inv_freq: expected float32")
-        _need(inv_freq, 2 * d, "inv_freq")
-        fr = _dptr(inv_freq)
-    if seqs is not None:
-        sq = _ints(seqs, T, "seqs")
-    args = _KV_STORE_ARGS.pack(qp, kp, vp, _ints(positions, T, "positions"), sq, qw, kw, fr, _dptr(q_out), _dptr(k_cache),
-                               _dptr(v_cache), qs, ks, vs, T, H, G, d, B, L, weight_offset, eps, _dtype_code(q), kv_format)
+    args = _KV_STORE_ARGS.pack(
+        qp, kp, vp, _ints(positions, T, "positions"), 0 if seqs is None else _ints(seqs, T, "seqs"),
+        0 if q_weight is None else _ptr(q_weight, 2 * d, "q_weight"),
+        0 if k_weight is None else _ptr(k_weight, 2 * d, "k_weight"),
+        0 if inv_freq is None else _ptr(inv_freq, 2 * d, "inv_freq"), _ptr(q_out, 2 * T * H * d, "q_out"),
+        _ptr(k_cache, cache, "k_cache"), _ptr(v_cache, cache, "v_cache"), qs, ks, vs, T, H, G, d, B, L, weight_offset, eps,
+        _dtype_code(q), kv_format)
     _check(lib.q4nx_kv_store(args, _stream(stream)), "q4nx_kv_store")
 
 
@@ -495,15 +497,13 @@ def q4nx_kv4_load(k_cache, v_cache, positions, k_out, v_out, T: int, G: int, d: 
                   stream=None):
     """k_out, v_out [T][G][d] (float32 or bfloat16) <- the values of rows (seqs[t], positions[t]) of 4-bit caches."""
     cache = _cache_bytes(B, G, d, L, Q4NX_KV_Q4)
-    _need(k_cache, cache, "k_cache")
-    _need(v_cache, cache, "v_cache")
     if v_out.dtype != k_out.dtype:
         raise ValueError("k_out and v_out must share one dtype")
-    _need(k_out, T * G * d * k_out.element_size(), "k_out")
-    _need(v_out, T * G * d * v_out.element_size(), "v_out")
-    _check(lib.q4nx_kv4_load(_dptr(k_cache), _dptr(v_cache), _ints(positions, T, "positions"),
-                             None if seqs is None else _ints(seqs, T, "seqs"), T, G, d, B, L, _dptr(k_out), _dptr(v_out),
-                             _dtype_code(k_out), _stream(stream)), "q4nx_kv4_load")
+    rows = T * G * d * k_out.element_size()
+    _check(lib.q4nx_kv4_load(_ptr(k_cache, cache, "k_cache"), _ptr(v_cache, cache, "v_cache"),
+                             _ints(positions, T, "positions"), None if seqs is None else _ints(seqs, T, "seqs"), T, G, d,
+                             B, L, _ptr(k_out, rows, "k_out"), _ptr(v_out, rows, "v_out"), _dtype_code(k_out),
+                             _stream(stream)), "q4nx_kv4_load")
 
 
 def q4nx_kv4_workspace_size(B: int, T: int, H: int, G: int, d: int, L: int, window: int = 0) -> int:
@@ -515,11 +515,9 @@ def q4nx_kv4_attention(q, k_cache, v_cache, lens, B: int, T: int, H: int, G: int
     """o[B][T][H][d] <- attention of the queries q[B][T][H][d], the last T positions of sequences of lens[b] positions,
     over 4-bit caches (window 0 = full attention)."""
     cache = _cache_bytes(B, G, d, L, Q4NX_KV_Q4)
-    _need(q, 2 * B * T * H * d, "q")
-    _need(k_cache, cache, "k_cache")
-    _need(v_cache, cache, "v_cache")
-    _need(o, B * T * H * d * o.element_size(), "o")
+    n = B * T * H * d
     wp, wn = (None, 0) if work is None else (_dptr(work), work.nbytes)
-    _check(lib.q4nx_kv4_attention(_dptr(q), _dptr(k_cache), _dptr(v_cache), _ints(lens, B, "lens"), B, T, H, G, d, L,
-                                  window, scale, _dptr(o), _dtype_code(o), wp, wn, _stream(stream)),
+    _check(lib.q4nx_kv4_attention(_ptr(q, 2 * n, "q"), _ptr(k_cache, cache, "k_cache"), _ptr(v_cache, cache, "v_cache"),
+                                  _ints(lens, B, "lens"), B, T, H, G, d, L, window, scale,
+                                  _ptr(o, n * o.element_size(), "o"), _dtype_code(o), wp, wn, _stream(stream)),
            "q4nx_kv4_attention")

@@ -220,7 +220,33 @@ __global__ __launch_bounds__(256) void kv_store_kernel(StoreArgs a) {
     }
   }
 
-  const int blk = pos >> 5, pa = (pos >> 4) & 1, ph = (pos >> 2) & 3, pr = pos & 3;
+  // Where the lane's first head goes; a step's heads lie RW rows on.  Of a 4-bit
+  // cache: the codes of the lane's first group, and that group's pair (of lanes
+  // that write one).
+  const int u = j & 7, g0 = j >> 3;  // groups g0 and g0 + D / 64
+  const int64_t head0 = (int64_t)seq * a.G + h0 + sub;
+  uint16_t* out16 = nullptr;
+  uint8_t* codes = nullptr;
+  uint32_t* pairs = nullptr;
+  int64_t next = 0;
+  if (kind == 0) {
+    out16 = a.q_out + ((int64_t)t * a.H + h0 + sub) * D + 4 * j;
+    next = RW * D;
+  } else {
+    uint8_t* const cache = kind == 1 ? a.k_cache : a.v_cache;
+    if constexpr (!Q4) {
+      out16 = reinterpret_cast<uint16_t*>(cache) + (head0 * a.P + pos) * D + 4 * j;
+      next = RW * a.P * D;
+    } else {
+      const int blk = pos >> 5, pa = (pos >> 4) & 1, ph = (pos >> 2) & 3, pr = pos & 3;
+      codes = cache + head0 * a.P * (D / 2) +
+              (kind == 1 ? (int64_t)pos * (D / 2) + 16 * g0 + 2 * u
+                         : (int64_t)blk * (16 * D) + (g0 >> 1) * 1024 + (ph * 16 + 4 * u) * 16 + (g0 & 1) * 8 + pa * 4 + pr);
+      pairs = reinterpret_cast<uint32_t*>(cache + a.heads_P * (D / 2)) + head0 * a.P * (D / 32) +
+              (kind == 1 ? (int64_t)pos * (D / 32) + g0 : (int64_t)blk * D + g0 * 32 + ph * 8 + pa * 4 + pr);
+      next = RW * a.P;
+    }
+  }
   const auto step = [&](int s, f32x4 x, f32x4 y) __attribute__((always_inline)) {
     const int h = h0 + s * RW + sub;
     const bool there = h < heads;
@@ -253,46 +279,44 @@ __global__ __launch_bounds__(256) void kv_store_kernel(StoreArgs a) {
       x *= A;
       y *= C;
     }
-    if (kind == 0) {
+    if (!Q4 || kind == 0) {
       if (there) {
-        uint16_t* const o = a.q_out + ((int64_t)t * a.H + h) * D + 4 * j;
-        *reinterpret_cast<uint2*>(o) = bf16x4_bits(x);
-        *reinterpret_cast<uint2*>(o + D / 2) = bf16x4_bits(y);
+        *reinterpret_cast<uint2*>(out16) = bf16x4_bits(x);
+        *reinterpret_cast<uint2*>(out16 + D / 2) = bf16x4_bits(y);
       }
+      out16 += next;
       return;
     }
-    const int64_t head = (int64_t)seq * a.G + min(h, heads - 1);
-    uint8_t* const cache = kind == 1 ? a.k_cache : a.v_cache;
-    if constexpr (!Q4) {
-      if (there) {
-        uint16_t* const o = reinterpret_cast<uint16_t*>(cache) + (head * a.P + pos) * D + 4 * j;
-        *reinterpret_cast<uint2*>(o) = bf16x4_bits(x);
-        *reinterpret_cast<uint2*>(o + D / 2) = bf16x4_bits(y);
-      }
-    } else {
+    if constexpr (Q4) {
       uint32_t pair[2], code[2] = {group_codes(x, pair[0]), group_codes(y, pair[1])};
-      const int u = j & 7, g0 = j >> 3;  // groups g0 and g0 + D / 64
-      uint32_t* const pairs = reinterpret_cast<uint32_t*>(cache + a.heads_P * (D / 2)) + head * a.P * (D / 32);
-      uint8_t* const codes = cache + head * a.P * (D / 2);
+      if (kind == 1) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int g = g0 + i * (D / 64);
-        if (kind == 1) {
-          const uint32_t odd = (uint32_t)xor_lane_bits<1>((int)code[i]);
-          if (there && (u & 1) == 0)
-            *reinterpret_cast<uint32_t*>(codes + (int64_t)pos * (D / 2) + 16 * g + 2 * u) = code[i] | (odd << 4);
-          if (there && u == 0) pairs[(int64_t)pos * (D / 32) + g] = pair[i];
-        } else {
-          const uint32_t both = code[i] | ((uint32_t)xor_lane_bits<4>((int)code[i]) << 4);
-          if (there && u < 4) {
-            uint8_t* const o = codes + (int64_t)blk * (16 * D) + (g >> 1) * 1024 + (ph * 16 + 4 * u) * 16 + (g & 1) * 8 +
-                               pa * 4 + pr;
+        for (int i = 0; i < 2; ++i) code[i] |= (uint32_t)xor_lane_bits<1>((int)code[i]) << 4;  // values 4 on: the lane beside
+        if (there && (u & 1) == 0) {
+          *reinterpret_cast<uint32_t*>(codes) = code[0];
+          *reinterpret_cast<uint32_t*>(codes + 16 * (D / 64)) = code[1];
+        }
+        if (there && u == 0) {
+          pairs[0] = pair[0];
+          pairs[D / 64] = pair[1];
+        }
+      } else {
+        constexpr int kFar = D == 64 ? 8 : 1024 * (D / 128);  // from group g0's bytes to group g0 + D / 64's
 #pragma unroll
-            for (int b = 0; b < 4; ++b) o[16 * b] = (uint8_t)(both >> (8 * b));
-          }
-          if (there && u == 0) pairs[(int64_t)blk * D + g * 32 + ph * 8 + pa * 4 + pr] = pair[i];
+        for (int i = 0; i < 2; ++i) code[i] |= (uint32_t)xor_lane_bits<4>((int)code[i]) << 4;  // values 16 on: 4 lanes on
+        if (there && u < 4) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) codes[i * kFar + 16 * b] = (uint8_t)(code[i] >> (8 * b));
+        }
+        if (there && u == 0) {
+          pairs[0] = pair[0];
+          pairs[32 * (D / 64)] = pair[1];
         }
       }
+      codes += next * (D / 2);
+      pairs += next * (D / 32);
     }
   };
 #pragma unroll 1
@@ -755,7 +779,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void kv4_merge_kernel(AttnArgs a,
 //   V  [B G][block][D/32 i][2 s][2 h][32 m][8 e]: value 32i + m of position
 //      16s + 8 (e / 4) + 4h + e % 4, where the score product of 32 positions
 //      leaves the weights of lane half h
-// Positions that no row attends to are zeros.
+// Positions that no row attends to are zeros.  grid (blocks, B G, K and V).
 constexpr int kExpandGroups = 2048;
 
 // The first block that any row of the sequence attends to.
@@ -778,37 +802,40 @@ __global__ __launch_bounds__(256) void kv4_expand_kernel(AttnArgs a, u32x4* __re
     const int p0 = (base + blk) * kKvBlock;
     u32x4* kd = ko + ((int64_t)bg * cap + blk) * (4 * D);
     u32x4* vd = vo + ((int64_t)bg * cap + blk) * (4 * D);
+    if (blockIdx.z == 0) {
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-      const int e = i * 256 + threadIdx.x, c = e >> 6, h = (e >> 5) & 1, p = p0 + (e & 31);
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(kc + (int64_t)p * (D / 2) + 8 * c + 4 * h);
-      const uint32_t pr = kp[(int64_t)p * (D / 32) + c / 2];
-      const u32x4 v = k_operand(w, bf16_to_f32(pr & 0xFFFFu) * 512.0f, __uint_as_float(pr & 0xFFFF0000u));
-      kd[e] = p >= j0 && p < len ? v : (u32x4){0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-      const int e = i * 256 + threadIdx.x, t = e >> 7, s = (e >> 6) & 1, h = (e >> 5) & 1, m = e & 31;
-      u32x4 o;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int hh = 2 * k + h;  // the layout's lane group: positions 16s + 4hh + r
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(vc + (int64_t)(base + blk) * (16 * D) + (t >> 1) * 1024 +
-                                                              (hh * 16 + (m & 15)) * 16 + (t & 1) * 8 + s * 4);
-        u32x4 pr = *reinterpret_cast<const u32x4*>(vp + (int64_t)(base + blk) * D + t * 32 + hh * 8 + s * 4);
-        float d[4], mm[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int p = p0 + 16 * s + 4 * hh + r;
-          if (p < j0 || p >= len) pr[r] = 0;
-          d[r] = bf16_to_f32(pr[r] & 0xFFFFu);
-          mm[r] = __uint_as_float(pr[r] & 0xFFFF0000u);
-        }
-        const uint2 x = v_operand((m & 16 ? w >> 4 : w) & 0x0F0F0F0Fu, d, mm);
-        o[2 * k] = x.x;
-        o[2 * k + 1] = x.y;
+      for (int i = 0; i < D / 64; ++i) {
+        const int e = i * 256 + threadIdx.x, c = e >> 6, h = (e >> 5) & 1, p = p0 + (e & 31);
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(kc + (int64_t)p * (D / 2) + 8 * c + 4 * h);
+        const uint32_t pr = kp[(int64_t)p * (D / 32) + c / 2];
+        const u32x4 v = k_operand(w, bf16_to_f32(pr & 0xFFFFu) * 512.0f, __uint_as_float(pr & 0xFFFF0000u));
+        kd[e] = p >= j0 && p < len ? v : (u32x4){0, 0, 0, 0};
       }
-      vd[e] = o;
+    } else {
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const int e = i * 256 + threadIdx.x, t = e >> 7, s = (e >> 6) & 1, h = (e >> 5) & 1, m = e & 31;
+        u32x4 o;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int hh = 2 * k + h;  // the layout's lane group: positions 16s + 4hh + r
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(vc + (int64_t)(base + blk) * (16 * D) + (t >> 1) * 1024 +
+                                                                (hh * 16 + (m & 15)) * 16 + (t & 1) * 8 + s * 4);
+          u32x4 pr = *reinterpret_cast<const u32x4*>(vp + (int64_t)(base + blk) * D + t * 32 + hh * 8 + s * 4);
+          float d[4], mm[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int p = p0 + 16 * s + 4 * hh + r;
+            if (p < j0 || p >= len) pr[r] = 0;
+            d[r] = bf16_to_f32(pr[r] & 0xFFFFu);
+            mm[r] = __uint_as_float(pr[r] & 0xFFFF0000u);
+          }
+          const uint2 x = v_operand((m & 16 ? w >> 4 : w) & 0x0F0F0F0Fu, d, mm);
+          o[2 * k] = x.x;
+          o[2 * k + 1] = x.y;
+        }
+        vd[e] = o;
+      }
     }
   }
 }
@@ -954,20 +981,20 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
   if (steps > 0) {
     copy(ksrc, 0, 0);
     copy(ksrc, 0, 1);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    copy(vsrc, 1, 0);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kCopies) : "memory");  // K of both steps
     const u32x4* const k0 = operands(0, 0);
     const u32x4* const k1 = operands(0, 1);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) kf[c] = k1[c * 64];
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.0f;
 #pragma unroll
     for (int c = 0; c < NC; ++c) s = mfma32(k0[c * 64], qf[c], s);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) kf[c] = k1[c * 64];
-    __syncthreads();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // every wave has read them
     copy(ksrc, 0, 2);
-    copy(vsrc, 1, 0);
     copy(ksrc, 0, 3);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies) : "memory");  // all but the last, for the first step's barriers
   }
   // Step i: the weights and outputs of scores s, and the scores sn of the next
   // step (of the last step: of whatever is there) from kf, which takes K of
@@ -1164,7 +1191,7 @@ static void launch_attention(const AttnArgs& a, const AttnPlan& p, int64_t BG, b
   if (p.rw) {
     u32x4* kx = reinterpret_cast<u32x4*>(a.work);
     const int64_t x = std::min(p.cap, std::max<int64_t>(1, kExpandGroups / BG));
-    hipLaunchKernelGGL((kv4_expand_kernel<D>), dim3((unsigned)x, (unsigned)BG), dim3(256), 0, stream, a, kx,
+    hipLaunchKernelGGL((kv4_expand_kernel<D>), dim3((unsigned)x, (unsigned)BG, 2), dim3(256), 0, stream, a, kx,
                        kx + (BG * p.cap + 1) * (4 * D), (int)p.cap);
     if (p.rw == 4) bf16 ? launch_tiles<D, 4, 1, 1>(a, p, BG, stream) : launch_tiles<D, 4, 1, 3>(a, p, BG, stream);
     else bf16 ? launch_tiles<D, 2, 2, 1>(a, p, BG, stream) : launch_tiles<D, 2, 2, 3>(a, p, BG, stream);
@@ -1180,7 +1207,7 @@ static void launch_attention(const AttnArgs& a, const AttnPlan& p, int64_t BG, b
 }
 
 // ---- launchers ------------------------------------------------------------
-constexpr int64_t kStoreWaves = 16384;
+constexpr int64_t kStoreWaves = 8192;
 template <int D, bool F32, bool Q4>
 static void launch_store(const StoreArgs& a, hipStream_t stream) {
   const int64_t groups = ceil_div((int64_t)a.T * (a.q_parts + 2 * a.kv_parts), 4 * kXcds) * kXcds;
