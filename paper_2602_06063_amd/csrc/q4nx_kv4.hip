@@ -403,7 +403,7 @@ struct AttnArgs {
   int T, H, G, L, window, rows;  // rows = T H / G of a KV group
   int hg, splits;
   float scale2;                  // scale * log2(e)
-  uint32_t by_hg, by_G, by_waves;  // reciprocals of hg, G and the waves of all splits (see over)
+  uint32_t by_hg, by_G, by_parts;  // reciprocals of hg, G and the parts of a range (waves of all splits, or splits; see over)
 };
 
 // x / n by a multiplication with 2^32 / n rounded up (0 for n = 1): exact for
@@ -433,7 +433,7 @@ __device__ __forceinline__ TileRange tile_range(const AttnArgs& a, int b, int ti
   r.j0 = a.window ? max(0, max(0, r.len - a.T + r.t0) - a.window + 1) : 0;
   r.blk0 = r.j0 / kKvBlock;
   r.nblk = r.j1 > r.j0 ? (r.j1 + kKvBlock - 1) / kKvBlock - r.blk0 : 0;
-  r.per = max(1, over(r.nblk + a.splits * kAttnWaves - 1, a.by_waves));
+  r.per = max(1, over(r.nblk + a.splits * kAttnWaves - 1, a.by_parts));
   return r;
 }
 __device__ __forceinline__ int active_splits(const TileRange& r) {
@@ -704,28 +704,66 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
   }
 }
 
-// Merges the splits of a row: workgroup (row of a group, B G, 64 values).  Each
-// of the 8 waves takes every eighth split, eight at a time (one round trip to
-// memory), with a running maximum; the waves' states are merged in order.
+// Blocks of 32 positions for rows t0 .. t1 of a sequence (none if nblk = 0).
+struct BlockRange {
+  int blk0, nblk;
+};
+__device__ __forceinline__ BlockRange block_range(const AttnArgs& a, int len, int t0, int t1) {
+  const int hi = len - a.T + t1;
+  const int lo = a.window ? max(0, max(0, len - a.T + t0) - a.window + 1) : 0;
+  return {lo / kKvBlock, hi >= lo ? hi / kKvBlock + 1 - lo / kKvBlock : 0};
+}
+
+// How a workgroup of kv4_tiles_kernel shares the blocks of its tile: splits of
+// at least kTileBlocks blocks, an even number.
+constexpr int kTileBlocks = 16;
+struct TileSplit {
+  int per, active;
+};
+__device__ __forceinline__ TileSplit tile_split(const AttnArgs& a, int nblk) {
+  TileSplit s;
+  s.per = max(kTileBlocks, (over(nblk + a.splits - 1, a.by_parts) + 1) & ~1);
+  s.active = nblk <= s.per ? 1 : (nblk + s.per - 1) / s.per;
+  return s;
+}
+
+// Merges the splits of the rows that have more than one (the others the first
+// launch has written): partials [B G][tile][split][row of the tile][m, l, -, -,
+// D values].  A wave takes 64 values of a row, or 1 / `slices` of the splits of
+// them (slices waves, a power of two, then merge through LDS in order): every
+// slices-th split, eight at a time (one round trip to memory).
+// grid (8 / slices units of 64 values each, B G).
 constexpr int kMergeAhead = 8, kMergeWaves = 8;
-template <int D>
-__global__ __launch_bounds__(64 * kMergeWaves) void kv4_merge_kernel(AttnArgs a, int tiles, int bf16) {
+template <int D, bool TILES>
+__global__ __launch_bounds__(64 * kMergeWaves) void kv4_merge_kernel(AttnArgs a, const float* __restrict__ parts, int tiles,
+                                                                     int tile_rows, int slices, int bf16) {
   __shared__ float ys[kMergeWaves][64], ls[kMergeWaves], ms[kMergeWaves];
-  const int row = blockIdx.x, bg = blockIdx.y, b = over(bg, a.by_G), g = bg - b * a.G;
-  const int tile = row / kRowTile;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, dim = blockIdx.z * 64 + lane;
-  const TileRange r = tile_range(a, b, tile);
-  const int active = active_splits(r);
-  if (active <= 1) return;  // the first launch has written it
-  const float* part = a.work + (((int64_t)bg * tiles + tile) * a.splits * kRowTile + row % kRowTile) * (D + 4);
-  const int64_t step = (int64_t)kRowTile * (D + 4);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int slice = wave & (slices - 1), first = wave - slice;
+  const int unit = (blockIdx.x * kMergeWaves + wave) / slices;
+  const int row = unit / (D / 64), dim = (unit & (D / 64 - 1)) * 64 + lane;
+  const int bg = blockIdx.y, b = over(bg, a.by_G), g = bg - b * a.G;
+  int active = 0, tile = 0;
+  if (row < a.rows) {
+    tile = row / tile_rows;
+    if constexpr (TILES) {
+      const int len = min(max(a.lens[b], 0), a.L);
+      const int t0 = over(tile * tile_rows, a.by_hg), t1 = min(a.T - 1, over(tile * tile_rows + tile_rows - 1, a.by_hg));
+      active = tile_split(a, block_range(a, len, t0, t1).nblk).active;
+    } else {
+      active = active_splits(tile_range(a, b, tile));
+    }
+  }
+  if (active <= 1) active = 0;
+  const int64_t step = (int64_t)tile_rows * (D + 4);
+  const float* part = parts + (((int64_t)bg * tiles + tile) * a.splits * tile_rows + (row - tile * tile_rows)) * (D + 4);
   float m = -INFINITY, l = 0.0f, y = 0.0f;
-  for (int s0 = wave; s0 < active; s0 += kMergeWaves * kMergeAhead) {
+  for (int s0 = slice; s0 < active; s0 += slices * kMergeAhead) {
     float pm[kMergeAhead], pl[kMergeAhead], py[kMergeAhead];
 #pragma unroll
     for (int k = 0; k < kMergeAhead; ++k) {
-      const bool in = s0 + kMergeWaves * k < active;
-      const float* p = part + (in ? s0 + kMergeWaves * k : s0) * step;
+      const bool in = s0 + slices * k < active;
+      const float* p = part + (in ? s0 + slices * k : s0) * step;
       pm[k] = in ? p[0] : -INFINITY;
       pl[k] = p[1];
       py[k] = p[4 + dim];
@@ -744,25 +782,29 @@ __global__ __launch_bounds__(64 * kMergeWaves) void kv4_merge_kernel(AttnArgs a,
       y = fmaf(c, py[k], y);
     }
   }
-  ys[wave][lane] = y;
-  if (lane == 0) {
-    ms[wave] = m;
-    ls[wave] = l;
-  }
-  __syncthreads();
-  if (wave == 0) {
-    float mx = ms[0];
-#pragma unroll
-    for (int w = 1; w < kMergeWaves; ++w) mx = fmaxf(mx, ms[w]);
-    const float base = mx == -INFINITY ? 0.0f : mx;
-    float lt = 0.0f, yt = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kMergeWaves; ++w) {
-      const float c = __builtin_amdgcn_exp2f(ms[w] - base);
-      lt = fmaf(c, ls[w], lt);
-      yt = fmaf(c, ys[w][lane], yt);
+  if (slices > 1) {  // the same for every wave
+    ys[wave][lane] = y;
+    if (lane == 0) {
+      ms[wave] = m;
+      ls[wave] = l;
     }
-    const float o = lt == 0.0f ? 0.0f : yt / lt;
+    __syncthreads();
+    if (slice == 0 && active) {
+      float mx = m;
+      for (int w = 1; w < slices; ++w) mx = fmaxf(mx, ms[first + w]);
+      const float base = mx == -INFINITY ? 0.0f : mx;
+      const float c0 = __builtin_amdgcn_exp2f(m - base);
+      l *= c0;
+      y *= c0;
+      for (int w = 1; w < slices; ++w) {
+        const float c = __builtin_amdgcn_exp2f(ms[first + w] - base);
+        l = fmaf(c, ls[first + w], l);
+        y = fmaf(c, ys[first + w][lane], y);
+      }
+    }
+  }
+  if (slice == 0 && active) {
+    const float o = l == 0.0f ? 0.0f : y / l;
     const int t = over(row, a.by_hg);
     const int64_t i = (((int64_t)b * a.T + t) * a.H + g * a.hg + row - t * a.hg) * D + dim;
     if (bf16) static_cast<uint16_t*>(a.o)[i] = f32_to_bf16_bits(o);
@@ -886,7 +928,7 @@ __device__ __forceinline__ void copy_one(const u32x4* src, const uint32_t (&offs
 // takes the exponentials of this one, so that the matrix unit works under the
 // vector unit's share of the step: K is a step ahead of V.
 //
-// grid: tiles with the longest ranges first, neighbours of one another on
+// grid (tiles, splits): tiles with the longest ranges first, neighbours of one another on
 // different groups, so that each XCD (workgroups are dealt out to the 8 in
 // turn) works on few groups at a time.
 // Orders what stands between scheduling barriers: N times a matrix
@@ -905,7 +947,8 @@ __device__ __forceinline__ void interleave() {
 
 template <int D, int RW, int KS, int NP>
 __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kernel(AttnArgs a, const u32x4* __restrict__ kx,
-                                                                                   const u32x4* __restrict__ vx, int cap,
+                                                                                   const u32x4* __restrict__ vx,
+                                                                                   float* __restrict__ parts, int cap,
                                                                                    int tiles, int BG) {
   constexpr int W = RW * KS, NC = D / 16, NT = D / 32, kRows = 32 * RW;
   constexpr int kVec = 4 * D;  // 16-byte pieces of a block
@@ -925,13 +968,17 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
   const int t = there ? over(row, a.by_hg) : a.T - 1;
   const int64_t q_row = ((int64_t)b * a.T + t) * a.H + g * a.hg + (there ? row - t * a.hg : 0);
   const int row_hi = first + t, row_lo = a.window ? row_hi - a.window + 1 : 0;
-  // Positions of the workgroup's rows, and what all the wave's rows see.
-  const int wg_hi = __builtin_amdgcn_readfirstlane(first + min(a.T - 1, over(tile * kRows + kRows - 1, a.by_hg)));
-  const int wg_lo = __builtin_amdgcn_readfirstlane(a.window ? max(0, max(0, first + over(tile * kRows, a.by_hg)) - a.window + 1) : 0);
+  // The blocks of the workgroup's split of the tile, and what all the wave's
+  // rows see.
+  const int base = __builtin_amdgcn_readfirstlane(first_block(a, len));
+  const BlockRange all = block_range(a, len, over(tile * kRows, a.by_hg), min(a.T - 1, over(tile * kRows + kRows - 1, a.by_hg)));
+  const TileSplit split = tile_split(a, all.nblk);
+  const int at = blockIdx.y * split.per;
+  if (blockIdx.y > 0 && at >= all.nblk) return;  // the whole workgroup
+  const int blk0 = __builtin_amdgcn_readfirstlane(all.blk0 + at);
+  const int nblk = __builtin_amdgcn_readfirstlane(min(all.nblk - at, split.per));
   const int hi_min = __builtin_amdgcn_readfirstlane(first + min(over(r0, a.by_hg), a.T - 1));
   const int lo_max = __builtin_amdgcn_readfirstlane(a.window ? first + min(a.T - 1, over(r0 + 31, a.by_hg)) - a.window + 1 : 0);
-  const int base = __builtin_amdgcn_readfirstlane(first_block(a, len));
-  const int blk0 = wg_lo / kKvBlock, nblk = wg_hi >= wg_lo ? wg_hi / kKvBlock + 1 - blk0 : 0;
   const u32x4* ksrc = kx + ((int64_t)bg * cap + blk0 - base) * kVec;
   const u32x4* vsrc = vx + ((int64_t)bg * cap + blk0 - base) * kVec;
 
@@ -1133,7 +1180,22 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
     }
     if (ks > 0) return;
   }
-  if (there) {
+  if (!there) return;
+  if (split.active > 1) {
+    float* const part = parts + ((((int64_t)bg * tiles + tile) * a.splits + blockIdx.y) * kRows + 32 * rw + n) * (D + 4);
+#pragma unroll
+    for (int k = 0; k < NT; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4*>(part + 4 + 32 * k + 8 * e + 4 * half) =
+            (f32x4){y[k][4 * e], y[k][4 * e + 1], y[k][4 * e + 2], y[k][4 * e + 3]};
+    if (half == 0) {
+      part[0] = m;
+      part[1] = l;
+    }
+    return;
+  }
+  {
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // a row that attends to nothing is zero
 #pragma unroll
     for (int k = 0; k < NT; ++k)
@@ -1147,43 +1209,55 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
 // How a call runs.  Few rows: kv4_rows_kernel, about two workgroups per CU,
 // none with less than a block of positions for each wave at the longest range
 // that the call allows (lengths are known on the device only).  From
-// kTileRows rows of a group on: kv4_expand_kernel and kv4_tiles_kernel.
+// tile_rows_from rows of a group on: kv4_expand_kernel and kv4_tiles_kernel, a range split over
+// workgroups where there are fewer tiles than they can be.  Measured, all
+// launches of each side: d = 256, 4 groups, 128 rows over 4096 positions 25 us
+// as few rows and 35 as tiles, over 32768 83 and 109; 256 rows 37 and 36, 151
+// and 122.  d = 128, 16 groups, 128 rows 29 and 32, 162 and 160; 256 rows 50 and
+// 40, 317 and 195.  d = 64, 16 groups, 128 rows 20 and 23, 97 and 88.
+// Tiles of 128 rows (every operand read by 4 waves) from 512 of them on, else of
+// 64 with two key parts: d = 128, 16 groups, a prompt of 2048 tokens (512 tiles)
+// 54 us as 128 and 52 as 64 rows, 3000 tokens 87 and 95, 1024 tokens 29 and 21;
+// d = 256, 4 groups, 2048 tokens (128 tiles) 90 and 52.
 constexpr int kAttnGroups = 512;
-constexpr int64_t kTileRows = 96;
+static int64_t tile_rows_from(int64_t d) { return d == 256 ? 256 : 192; }
 struct AttnPlan {
   int64_t rows, tiles;
-  int splits;      // of the few rows' launch
+  int splits;
   int rw;          // waves of 32 rows in a tile; 0: few rows
   int64_t cap;     // expanded blocks of a (sequence, group)
+  size_t parts_at, bytes;  // of the workspace: where the partials begin, all of it
 };
-static AttnPlan attn_plan(int64_t B, int64_t T, int64_t H, int64_t G, int64_t L, int64_t window) {
+static AttnPlan attn_plan(int64_t B, int64_t T, int64_t H, int64_t G, int64_t d, int64_t L, int64_t window) {
   AttnPlan p = {};
+  const int64_t BG = B * G;
   p.rows = T * (H / G);
-  p.splits = 1;
-  if (p.rows >= kTileRows) {
+  int64_t tile_rows = kRowTile;
+  if (p.rows >= tile_rows_from(d)) {
     const int64_t span = window ? std::min(L, window - 1 + T) : L;
     p.cap = std::min(ceil_div(span, kKvBlock) + 1, kv_positions(L) / kKvBlock);
-    p.rw = B * G * ceil_div(p.rows, 128) >= 512 ? 4 : 2;
-    p.tiles = ceil_div(p.rows, 32 * p.rw);
-    return p;
+    p.rw = BG * ceil_div(p.rows, 128) >= 512 ? 4 : 2;
+    tile_rows = 32 * p.rw;
+    p.tiles = ceil_div(p.rows, tile_rows);
+    p.splits = (int)std::max<int64_t>(1, std::min((d == 256 ? 256 : 512) / (BG * p.tiles), ceil_div(p.cap, kTileBlocks)));
+    p.parts_at = (size_t)(BG * p.cap + 1) * (size_t)(2 * kKvBlock * d * 2);  // (a step may copy a block past the last)
+  } else {
+    p.tiles = ceil_div(p.rows, kRowTile);
+    const int64_t span = window ? std::min(L, window + std::min<int64_t>(T, kRowTile)) : L;
+    const int64_t blocks = ceil_div(span, kKvBlock) + 1;
+    p.splits = (int)std::max<int64_t>(1, std::min(kAttnGroups / (BG * p.tiles), ceil_div(blocks, kAttnWaves)));
   }
-  p.tiles = ceil_div(p.rows, kRowTile);
-  const int64_t span = window ? std::min(L, window + std::min<int64_t>(T, kRowTile)) : L;
-  const int64_t blocks = ceil_div(span, kKvBlock) + 1;
-  p.splits = (int)std::max<int64_t>(1, std::min(kAttnGroups / (B * G * p.tiles), ceil_div(blocks, kAttnWaves)));
+  p.bytes = p.parts_at + (p.splits == 1 ? 0 : (size_t)(BG * p.tiles * p.splits * tile_rows * (d + 4)) * sizeof(float));
   return p;
-}
-static size_t attn_work_bytes(const AttnPlan& p, int64_t BG, int64_t d) {
-  if (p.rw) return (size_t)(BG * p.cap + 1) * (size_t)(2 * kKvBlock * d * 2);  // (a step may copy a block past the last)
-  return p.splits == 1 ? 0 : (size_t)(BG * p.tiles * p.splits * kRowTile * (d + 4)) * sizeof(float);
 }
 
 template <int D, int RW, int KS, int NP>
 static void launch_tiles(const AttnArgs& a, const AttnPlan& p, int64_t BG, hipStream_t stream) {
   u32x4* kx = reinterpret_cast<u32x4*>(a.work);
   u32x4* vx = kx + (BG * p.cap + 1) * (4 * D);
-  hipLaunchKernelGGL((kv4_tiles_kernel<D, RW, KS, NP>), dim3((unsigned)(BG * p.tiles)), dim3(64 * RW * KS), 0, stream, a,
-                     kx, vx, (int)p.cap, (int)p.tiles, (int)BG);
+  hipLaunchKernelGGL((kv4_tiles_kernel<D, RW, KS, NP>), dim3((unsigned)(BG * p.tiles), (unsigned)p.splits),
+                     dim3(64 * RW * KS), 0, stream, a, kx, vx, a.work + p.parts_at / sizeof(float), (int)p.cap, (int)p.tiles,
+                     (int)BG);
 }
 
 template <int D>
@@ -1195,15 +1269,22 @@ static void launch_attention(const AttnArgs& a, const AttnPlan& p, int64_t BG, b
                        kx + (BG * p.cap + 1) * (4 * D), (int)p.cap);
     if (p.rw == 4) bf16 ? launch_tiles<D, 4, 1, 1>(a, p, BG, stream) : launch_tiles<D, 4, 1, 3>(a, p, BG, stream);
     else bf16 ? launch_tiles<D, 2, 2, 1>(a, p, BG, stream) : launch_tiles<D, 2, 2, 3>(a, p, BG, stream);
-    return;
+  } else {
+    const dim3 grid(p.splits, (unsigned)p.tiles, (unsigned)BG);
+    if (bf16) hipLaunchKernelGGL((kv4_rows_kernel<D, 2>), grid, dim3(64 * kAttnWaves), 0, stream, a);
+    else hipLaunchKernelGGL((kv4_rows_kernel<D, 3>), grid, dim3(64 * kAttnWaves), 0, stream, a);
   }
-  const dim3 grid(p.splits, (unsigned)p.tiles, (unsigned)BG);
-  if (bf16) hipLaunchKernelGGL((kv4_rows_kernel<D, 2>), grid, dim3(64 * kAttnWaves), 0, stream, a);
-  else hipLaunchKernelGGL((kv4_rows_kernel<D, 3>), grid, dim3(64 * kAttnWaves), 0, stream, a);
-  if (p.splits > 1)
-    hipLaunchKernelGGL((kv4_merge_kernel<D>), dim3((unsigned)p.rows, (unsigned)BG, D / 64), dim3(64 * kMergeWaves), 0,
-                       stream, a,
-                       (int)p.tiles, (int)bf16);
+  if (p.splits == 1) return;
+  int slices = 1;
+  while (slices < kMergeWaves && slices * kMergeAhead < p.splits) slices *= 2;
+  const dim3 grid((unsigned)ceil_div(p.rows * (D / 64) * slices, kMergeWaves), (unsigned)BG);
+  const float* parts = a.work + p.parts_at / sizeof(float);
+  if (p.rw)
+    hipLaunchKernelGGL((kv4_merge_kernel<D, true>), grid, dim3(64 * kMergeWaves), 0, stream, a, parts, (int)p.tiles,
+                       32 * p.rw, slices, (int)bf16);
+  else
+    hipLaunchKernelGGL((kv4_merge_kernel<D, false>), grid, dim3(64 * kMergeWaves), 0, stream, a, parts, (int)p.tiles,
+                       kRowTile, slices, (int)bf16);
 }
 
 // ---- launchers ------------------------------------------------------------
@@ -1355,7 +1436,7 @@ static q4nx_status check_attention(int64_t B, int64_t T, int64_t H, int64_t G, i
 size_t q4nx_kv4_workspace_size(int64_t B, int64_t T, int64_t H, int64_t G, int64_t d, int64_t L, int64_t window) {
   clear_error();
   if (check_attention(B, T, H, G, d, L, window)) return 0;
-  return attn_work_bytes(attn_plan(B, T, H, G, L, window), B * G, d);
+  return attn_plan(B, T, H, G, d, L, window).bytes;
 }
 
 q4nx_status q4nx_kv4_attention(const uint16_t* d_q, const void* d_k, const void* d_v, const int32_t* d_lens, int64_t B,
@@ -1370,8 +1451,8 @@ q4nx_status q4nx_kv4_attention(const uint16_t* d_q, const void* d_k, const void*
   if (!aligned(d_q, 16) || !aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_o, 16) || !aligned(d_work, 16) ||
       !aligned(d_lens, 4))
     return fail(Q4NX_ERR_ALIGNMENT, f + ": q, caches, o and the workspace need 16-byte alignment, lens 4-byte");
-  const AttnPlan p = attn_plan(B, T, H, G, L, window);
-  const size_t need = attn_work_bytes(p, B * G, d);
+  const AttnPlan p = attn_plan(B, T, H, G, d, L, window);
+  const size_t need = p.bytes;
   if (need && !d_work) return fail(Q4NX_ERR_INVALID_ARG, f + ": NULL workspace");
   if (work_bytes < need) return fail(Q4NX_ERR_BUFFER_TOO_SMALL, f + ": workspace smaller than q4nx_kv4_workspace_size");
   AttnArgs a;
@@ -1393,7 +1474,7 @@ q4nx_status q4nx_kv4_attention(const uint16_t* d_q, const void* d_k, const void*
   a.splits = p.splits;
   a.by_hg = reciprocal(H / G);
   a.by_G = reciprocal(G);
-  a.by_waves = reciprocal((int64_t)p.splits * kAttnWaves);
+  a.by_parts = reciprocal(p.rw ? p.splits : (int64_t)p.splits * kAttnWaves);
   // A scale of zero (equal weights) becomes the smallest normal one, which
   // leaves any finite score below 2^-25 but a masked one at -inf.
   a.scale2 = scale * 1.4426950408889634f;
