@@ -459,7 +459,7 @@ __device__ __forceinline__ u32x4 k_operand(uint32_t w, float d512, float m) {
 }
 
 // Four codes (bytes) of V, each with the pair of its own position.
-__device__ __forceinline__ uint2 v_operand(uint32_t bytes, const float (&d)[4], const float (&m)[4]) {
+__device__ __forceinline__ uint2 v_operand(uint32_t bytes, f32x4 d, f32x4 m) {
   const uint32_t c = opaque(bytes);
   return make_uint2(pack_bf16x2(fmaf((float)(c & 0xFFu), d[0], m[0]), fmaf((float)((c >> 8) & 0xFFu), d[1], m[1])),
                     pack_bf16x2(fmaf((float)((c >> 16) & 0xFFu), d[2], m[2]), fmaf((float)(c >> 24), d[3], m[3])));
@@ -488,6 +488,7 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
   constexpr int kStride = D + 4;
   __shared__ __attribute__((aligned(16))) float ys[kAttnWaves][kRowTile][kStride];
   __shared__ float ms[kAttnWaves][kRowTile], ls[kAttnWaves][kRowTile];
+  __shared__ __attribute__((aligned(16))) float scales[kAttnWaves][D], offsets[kAttnWaves][D];  // V's of a wave's block
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, h = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int split = blockIdx.x, tile = blockIdx.y, bg = blockIdx.z, b = over(bg, a.by_G), g = bg - b * a.G;
@@ -522,7 +523,9 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
   const int w1 = min(r.blk0 + r.nblk, w0 + r.per);
 
   uint32_t kw[2][kWords], kpair[2][D == 256 ? 2 : 1];
-  u32x4 vw[D / 64], vpair[NG][2];
+  constexpr int kPairs = D / 64;  // of V's pairs, in their order in memory, to a lane
+  u32x4 vw[D / 64];
+  uint32_t vpair[kPairs];
   const auto load_k = [&](int blk) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -548,11 +551,18 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
 #pragma unroll
     for (int u = 0; u < D / 64; ++u)
       vw[u] = *reinterpret_cast<const u32x4*>(vc + (int64_t)blk * (16 * D) + u * 1024 + lane * 16);
+    const uint32_t* pp = vp + (int64_t)blk * D + kPairs * lane;
+    if constexpr (kPairs == 1) {
+      vpair[0] = *pp;
+    } else if constexpr (kPairs == 2) {
+      const uint2 w = *reinterpret_cast<const uint2*>(pp);
+      vpair[0] = w.x;
+      vpair[1] = w.y;
+    } else {
+      const u32x4 w = *reinterpret_cast<const u32x4*>(pp);
 #pragma unroll
-    for (int u = 0; u < NG; ++u)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        vpair[u][i] = *reinterpret_cast<const u32x4*>(vp + (int64_t)blk * D + u * 32 + h * 8 + i * 4);
+      for (int e = 0; e < 4; ++e) vpair[e] = w[e];
+    }
   };
 
   float m = -INFINITY, l = 0.0f;
@@ -621,31 +631,34 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
         }
       }
     }
-    // Rows of the block that no query row attends to hold anything: a pair of
-    // zeros makes them 0, whatever their codes.
+    // V's scales and offsets as floats in the wave's LDS slot, where the 16 lanes
+    // of a lane group read the ones they share.  (Each lane taking the pairs of
+    // its 8 positions apart itself was 64 of 454 vector instructions a block at
+    // d = 128, and held 32 registers.)  Rows of the block that no query row
+    // attends to hold anything: a pair of zeros makes them 0, whatever their codes.
     if (p0 < r.j0 || p0 + kKvBlock > r.j1) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int p = p0 + 16 * i + 4 * h + e;
-          if (p < r.j0 || p >= r.j1) {
-#pragma unroll
-            for (int u = 0; u < NG; ++u) vpair[u][i][e] = 0;
-          }
-        }
+      for (int e = 0; e < kPairs; ++e) {
+        const int at = (kPairs * lane + e) & 31;                     // [4 h][2 a][4 r]
+        const int p = p0 + 16 * ((at >> 2) & 1) + 4 * (at >> 3) + (at & 3);
+        if (p < r.j0 || p >= r.j1) vpair[e] = 0;
+      }
     }
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) {
+      scales[wave][kPairs * lane + e] = bf16_to_f32(vpair[e] & 0xFFFFu);
+      offsets[wave][kPairs * lane + e] = __uint_as_float(vpair[e] & 0xFFFF0000u);
+    }
+    // (A wave's LDS instructions are carried out in order; the fences keep the
+    // compiler from moving the accesses across.)
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
 #pragma unroll
     for (int u = 0; u < NG; ++u) {
       u32x4 lo, hi;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        float d[4], mm[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          d[e] = bf16_to_f32(vpair[u][i][e] & 0xFFFFu);
-          mm[e] = __uint_as_float(vpair[u][i][e] & 0xFFFF0000u);
-        }
+        const f32x4 d = *reinterpret_cast<const f32x4*>(&scales[wave][u * 32 + h * 8 + i * 4]);
+        const f32x4 mm = *reinterpret_cast<const f32x4*>(&offsets[wave][u * 32 + h * 8 + i * 4]);
         const uint32_t w = vw[u / 2][2 * (u & 1) + i];
         const uint2 x = v_operand(w & 0x0F0F0F0Fu, d, mm), z = v_operand((w >> 4) & 0x0F0F0F0Fu, d, mm);
         lo[2 * i] = x.x;
@@ -659,6 +672,7 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
         y[2 * u + 1] = mfma16(hi, pf[k], y[2 * u + 1]);
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     if (blk + 1 < w1) load_v(blk + 1);
   }
   l += xor_lane<16>(l);
@@ -864,7 +878,7 @@ __global__ __launch_bounds__(256) void kv4_expand_kernel(AttnArgs a, u32x4* __re
           const uint32_t w = *reinterpret_cast<const uint32_t*>(vc + (int64_t)(base + blk) * (16 * D) + (t >> 1) * 1024 +
                                                                 (hh * 16 + (m & 15)) * 16 + (t & 1) * 8 + s * 4);
           u32x4 pr = *reinterpret_cast<const u32x4*>(vp + (int64_t)(base + blk) * D + t * 32 + hh * 8 + s * 4);
-          float d[4], mm[4];
+          f32x4 d, mm;
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int p = p0 + 16 * s + 4 * hh + r;
