@@ -349,12 +349,13 @@ typedef struct q4nx_kv_store_args {
  * the caches keep their contents.  A token whose position lies outside 0..L-1
  * or whose sequence lies outside 0..B-1 is padding: nothing of it is written,
  * in q_out neither.  Two tokens of one call must not name the same row (the
- * row's contents are not defined if they do).  d is 64, 128 or 256; H, G, B
- * and B G lie in 1..65535, L in 1..2^30, T in 1..2^24.  Pointers are 16-byte
- * aligned, positions and seqs 4-byte.
+ * row's contents are not defined if they do), and apart from q_out = q nothing
+ * written may overlap anything else.  d is 64, 128 or 256; H, G, B and B G lie
+ * in 1..65535, L in 1..2^30, T in 1..2^24.  Pointers are 16-byte aligned,
+ * positions and seqs 4-byte.
  * Errors: Q4NX_ERR_INVALID_ARG (NULL pointer, unknown dtype or format,
- * weight_offset not finite, eps not finite or negative), Q4NX_ERR_SHAPE,
- * Q4NX_ERR_ALIGNMENT, Q4NX_ERR_HIP.
+ * weight_offset not finite, eps not finite or negative, q_out = q for float32
+ * or with gaps between rows), Q4NX_ERR_SHAPE, Q4NX_ERR_ALIGNMENT, Q4NX_ERR_HIP.
  */
 q4nx_status q4nx_kv_store(const q4nx_kv_store_args* args, hipStream_t stream);
 
@@ -362,7 +363,7 @@ q4nx_status q4nx_kv_store(const q4nx_kv_store_args* args, hipStream_t stream);
  * Device.  The values that rows of a 4-bit cache stand for: K and V of
  * (d_seqs[t], every group, d_positions[t]) to row t of d_k_out and d_v_out,
  * [T][G][d] of out_dtype (exact in both types).  Rows of padding (as in
- * q4nx_kv_store) are left as they were.  T * G is at most 2^32.
+ * q4nx_kv_store) are left as they were.  T G d is at most 2^34.
  * Errors: Q4NX_ERR_INVALID_ARG, Q4NX_ERR_SHAPE, Q4NX_ERR_ALIGNMENT, Q4NX_ERR_HIP.
  */
 q4nx_status q4nx_kv4_load(const void* d_k, const void* d_v, const int32_t* d_positions, const int32_t* d_seqs,
@@ -389,15 +390,20 @@ size_t q4nx_kv4_workspace_size(int64_t B, int64_t T, int64_t H, int64_t G, int64
  *   d_lens : device, [B] int32, 4-byte aligned; read as clamped to 0..L.  They
  *            may change from replay to replay of a captured call.
  *   H, G   : H a multiple of G, at most 16 G;  d: 64, 128 or 256
- *   T      : 1..L, T H/G at most 2^20 - 16;  window: 0..2^30
+ *   T      : 1..L, T H/G at most 2^20 - 16, B T H at most 2^30;  window: 0..2^30
  *   d_o    : device, [B][T][H][d] of o_dtype; fully written
  *   d_work : device, at least q4nx_kv4_workspace_size bytes, owned by the
  *            caller (NULL where that is 0); contents on entry do not matter.
- *            Calls that share a workspace must not overlap.
+ *            Calls that share a workspace must not overlap.  With few rows
+ *            it holds partial results (some MB); with many (T H/G from 192 on,
+ *            from 256 at d = 256) also K and V of the attended range in bf16,
+ *            4 d bytes a position of each sequence and group.
  * Pointers are 16-byte aligned where nothing else is said.  Scores are float32
- * sums of exact bf16 products, exponentials and sums float32; the weights of
- * the values are rounded so finely that a float32 output keeps float32
- * accuracy.  The order of the sums depends on B, T, H, G, d, L, window and the
+ * sums of exact bf16 products, exponentials and sums float32.  A weight of a
+ * value enters the product as a sum of bf16 terms: three for a float32 output,
+ * which keeps float32 accuracy; for a bf16 output two with few rows (2^-16 of
+ * the weight), and one with many (2^-8 at most, as the output's own rounding,
+ * and of either sign from position to position).  The order of the sums depends on B, T, H, G, d, L, window and the
  * lengths alone: the same call gives the same bits every time.
  * Errors: Q4NX_ERR_INVALID_ARG (NULL pointer, unknown dtype, non-finite
  * scale), Q4NX_ERR_SHAPE, Q4NX_ERR_ALIGNMENT, Q4NX_ERR_BUFFER_TOO_SMALL,

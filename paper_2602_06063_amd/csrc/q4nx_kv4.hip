@@ -1220,20 +1220,32 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
   }
 }
 
-// How a call runs.  Few rows: kv4_rows_kernel, about two workgroups per CU,
-// none with less than a block of positions for each wave at the longest range
-// that the call allows (lengths are known on the device only).  From
-// tile_rows_from rows of a group on: kv4_expand_kernel and kv4_tiles_kernel, a range split over
-// workgroups where there are fewer tiles than they can be.  Measured, all
-// launches of each side: d = 256, 4 groups, 128 rows over 4096 positions 25 us
-// as few rows and 35 as tiles, over 32768 83 and 109; 256 rows 37 and 36, 151
-// and 122.  d = 128, 16 groups, 128 rows 29 and 32, 162 and 160; 256 rows 50 and
-// 40, 317 and 195.  d = 64, 16 groups, 128 rows 20 and 23, 97 and 88.
+// How a call runs, by the longest range that it allows (lengths are known on
+// the device only).
+//
+// Few rows: kv4_rows_kernel, about two workgroups per CU, none with less than a
+// block of positions for each wave.  Up to kOneGroup values of blocks times d
+// one workgroup takes a tile's whole range and the merge falls away: at d = 256
+// 256 positions take 8.1 us in one launch, 6.0 + 2.7 and the gap in two (8.3
+// and 9.5 us a call, from the host); at d = 128 512 positions 8.3 and 4.8 + 2.9
+// (8.0 and 9.5), at d = 64 1024 positions 9.4 and 4.2 + 3.2 (9.1 and 9.6).
+// Beyond, the two launches win: at d = 256 512 positions are 12.6 and 9.5 us a
+// call.
+//
+// From tile_rows_from rows of a group on: kv4_expand_kernel and
+// kv4_tiles_kernel, a range split over workgroups where there are fewer tiles
+// than they can be.  Measured, all launches of each side: d = 256, 4 groups, 128
+// rows over 4096 positions 25 us as few rows and 35 as tiles, over 32768 83 and
+// 109; 256 rows 37 and 36, 151 and 122.  d = 128, 16 groups, 128 rows 29 and
+// 32, 162 and 160; 256 rows 50 and 40, 317 and 195.  d = 64, 16 groups, 128
+// rows 20 and 23, 97 and 88.
+//
 // Tiles of 128 rows (every operand read by 4 waves) from 512 of them on, else of
 // 64 with two key parts: d = 128, 16 groups, a prompt of 2048 tokens (512 tiles)
 // 54 us as 128 and 52 as 64 rows, 3000 tokens 87 and 95, 1024 tokens 29 and 21;
 // d = 256, 4 groups, 2048 tokens (128 tiles) 90 and 52.
 constexpr int kAttnGroups = 512;
+constexpr int64_t kOneGroup = 2048;
 static int64_t tile_rows_from(int64_t d) { return d == 256 ? 256 : 192; }
 struct AttnPlan {
   int64_t rows, tiles;
@@ -1244,6 +1256,7 @@ struct AttnPlan {
 };
 static AttnPlan attn_plan(int64_t B, int64_t T, int64_t H, int64_t G, int64_t d, int64_t L, int64_t window) {
   AttnPlan p = {};
+  p.splits = 1;
   const int64_t BG = B * G;
   p.rows = T * (H / G);
   int64_t tile_rows = kRowTile;
@@ -1258,8 +1271,9 @@ static AttnPlan attn_plan(int64_t B, int64_t T, int64_t H, int64_t G, int64_t d,
   } else {
     p.tiles = ceil_div(p.rows, kRowTile);
     const int64_t span = window ? std::min(L, window + std::min<int64_t>(T, kRowTile)) : L;
-    const int64_t blocks = ceil_div(span, kKvBlock) + 1;
-    p.splits = (int)std::max<int64_t>(1, std::min(kAttnGroups / (BG * p.tiles), ceil_div(blocks, kAttnWaves)));
+    const int64_t blocks = ceil_div(span, kKvBlock) + (window ? 1 : 0);
+    if (blocks * d > kOneGroup)
+      p.splits = (int)std::max<int64_t>(1, std::min(kAttnGroups / (BG * p.tiles), ceil_div(blocks, kAttnWaves)));
   }
   p.bytes = p.parts_at + (p.splits == 1 ? 0 : (size_t)(BG * p.tiles * p.splits * tile_rows * (d + 4)) * sizeof(float));
   return p;
@@ -1377,6 +1391,9 @@ q4nx_status q4nx_kv_store(const q4nx_kv_store_args* args, hipStream_t stream) {
   if (!aligned(s.q_weight, 16) || !aligned(s.k_weight, 16) || !aligned(s.inv_freq, 16) || !aligned(s.q_out, 16) ||
       !aligned(s.k_cache, 16) || !aligned(s.v_cache, 16) || !aligned(s.positions, 4) || !aligned(s.seqs, 4))
     return fail(Q4NX_ERR_ALIGNMENT, f + ": weights, inv_freq, q_out and caches need 16-byte alignment, positions and seqs 4-byte");
+  // In place a wave writes what it has read only if rows and types match.
+  if (s.q == s.q_out && (f32 || s.q_stride != s.H * s.d))
+    return fail(Q4NX_ERR_INVALID_ARG, f + ": q_out may be q only for bf16 rows without gaps");
   StoreArgs a;
   a.q = s.q;
   a.k = s.k;
@@ -1418,7 +1435,8 @@ q4nx_status q4nx_kv4_load(const void* d_k, const void* d_v, const int32_t* d_pos
   if (!aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_k_out, 16) || !aligned(d_v_out, 16) ||
       !aligned(d_positions, 4) || !aligned(d_seqs, 4))
     return fail(Q4NX_ERR_ALIGNMENT, f + ": caches and outputs need 16-byte alignment, positions and seqs 4-byte");
-  if (T * G > (int64_t(1) << 32)) return fail(Q4NX_ERR_SHAPE, f + ": T G must not exceed 2^32");
+  // (a launch has fewer than 2^32 threads in a dimension, and each takes 8 values)
+  if (T * G * d > (int64_t(1) << 34)) return fail(Q4NX_ERR_SHAPE, f + ": T G d must not exceed 2^34");
   const int64_t P = kv_positions(L);
   const dim3 grid((unsigned)(ceil_div(T * G * (d / 8), 256 * kXcds) * kXcds));
   const auto go = [&](auto dc, auto fc) {
@@ -1443,6 +1461,8 @@ static q4nx_status check_attention(int64_t B, int64_t T, int64_t H, int64_t G, i
   if (H % G != 0 || H / G > 16) return fail(Q4NX_ERR_SHAPE, f + ": H must be a multiple of G, at most 16 of it");
   if (T > L) return fail(Q4NX_ERR_SHAPE, f + ": T must not exceed L");
   if (T * (H / G) > 65535 * (int64_t)kRowTile) return fail(Q4NX_ERR_SHAPE, f + ": T H / G must not exceed 2^20 - 16");
+  // (a launch has fewer than 2^32 threads in a dimension, and 2 to a row)
+  if (B * T * H > (int64_t(1) << 30)) return fail(Q4NX_ERR_SHAPE, f + ": B T H must not exceed 2^30");
   if (window < 0 || window > kMaxL) return fail(Q4NX_ERR_SHAPE, f + ": window must lie in 0..2^30");
   return Q4NX_OK;
 }

@@ -47,6 +47,9 @@ def test_store_refusals():
         assert _store(**{name: A + 8}) == q4.Q4NX_ERR_ALIGNMENT, name
     for change in (dict(positions=A + 2), dict(seqs=A + 2), dict(q_stride=1028), dict(in_dtype=0, k_stride=514)):
         assert _store(**change) == q4.Q4NX_ERR_ALIGNMENT, change
+    # In place for float32 and for rows with gaps: a wave would write what another has yet to read.
+    for change in (dict(in_dtype=0), dict(q_stride=1032), dict(T=1, q_stride=2048)):
+        assert _store(**change) == q4.Q4NX_ERR_INVALID_ARG, change
     assert "q4nx_kv_store" in LIB.q4nx_last_error().decode()
 
 
@@ -58,7 +61,8 @@ def test_load_refusals():
     for name in ("k", "v", "positions", "ko", "vo"):
         assert _load(**{name: 0}) == q4.Q4NX_ERR_INVALID_ARG, name
     assert _load(dtype=3) == q4.Q4NX_ERR_INVALID_ARG
-    for change in (dict(T=0), dict(G=0), dict(d=32), dict(B=0), dict(L=0), dict(B=2, G=40000), dict(B=1, T=1 << 24, G=65535)):
+    for change in (dict(T=0), dict(G=0), dict(d=32), dict(B=0), dict(L=0), dict(B=2, G=40000), dict(B=1, T=1 << 24, G=65535),
+                   dict(T=(1 << 24), G=9), dict(T=(1 << 23), G=9, d=256)):
         assert _load(**change) == q4.Q4NX_ERR_SHAPE, change
     for change in (dict(k=A + 4), dict(v=A + 8), dict(ko=A + 2), dict(vo=A + 4), dict(positions=A + 1), dict(seqs=A + 2)):
         assert _load(**change) == q4.Q4NX_ERR_ALIGNMENT, change
@@ -74,7 +78,8 @@ def test_attention_refusals():
                    dict(scale=float("nan")), dict(work=0)):
         assert _attend(**change) == q4.Q4NX_ERR_INVALID_ARG, change
     for change in (dict(B=0), dict(T=0), dict(T=32769), dict(H=6), dict(H=68), dict(G=0), dict(d=512), dict(L=0),
-                   dict(window=-1), dict(window=(1 << 30) + 1), dict(B=20000), dict(T=1 << 20, L=1 << 30)):
+                   dict(window=-1), dict(window=(1 << 30) + 1), dict(B=20000), dict(T=1 << 20, L=1 << 30),
+                   dict(B=60000, H=1, G=1, T=20000), dict(B=16384, T=8193, H=8, G=1)):
         assert _attend(**change) == q4.Q4NX_ERR_SHAPE, change
     for change in (dict(q=A + 8), dict(k=A + 4), dict(v=A + 4), dict(o=A + 8), dict(work=A + 8), dict(lens=A + 2)):
         assert _attend(**change) == q4.Q4NX_ERR_ALIGNMENT, change

@@ -528,3 +528,115 @@ def test_other_stream_and_small_workspace(q4):
     for bad in (work[:need - 1], None):
         with pytest.raises(q4.Q4NXError):
             q4.q4nx_kv4_attention(q, *caches, lens, 1, 1, H, G, d, L, 0, 0.1, b, bad)
+
+
+def test_a_nan_query_stays_in_its_row(q4):
+    """A row of NaN or infinity leaves the rows that share its tile, its blocks and its maximum's test alone."""
+    print("[case] NaN query rows", flush=True)
+    rng = np.random.default_rng(21)
+    H, G, d, n = 8, 2, 128, 700
+    caches, _ = _cache(rng, q4, 1, G, d, n, [n])
+    for T in (1, 5, 60):                                                  # one tile, two, and tiles of 64 rows
+        q = _bf16(oracle.f32_to_bf16(rng.standard_normal((1, T, H, d)).astype(np.float32)))
+        bad = q.clone()
+        bad[0, T // 2, 1] = float("nan")
+        bad[0, 0, 6, 3] = float("inf")
+        work = torch.empty(max(16, q4.q4nx_kv4_workspace_size(1, T, H, G, d, n)), dtype=torch.uint8, device="cuda")
+        o = [torch.empty(1, T, H, d, device="cuda") for _ in range(2)]
+        for x, y in zip((q, bad), o):
+            q4.q4nx_kv4_attention(x, *caches, _ints([n]), 1, T, H, G, d, n, 0, 0.1, y, work)
+        assert torch.isnan(o[1][0, T // 2, 1]).all() and torch.isnan(o[1][0, 0, 6]).all() and torch.isfinite(o[0]).all()
+        keep = torch.ones(T, H, dtype=torch.bool, device="cuda")
+        keep[T // 2, 1] = keep[0, 6] = False
+        # (a maximum that one row moves is moved for all 16 or 32 of them, so the roundings of the others may differ)
+        tol = 4 * ((n + 64) * U + 2.0 ** -20) * 12                        # |v| < 12: 4 sigma, a spread of e^1, a step
+        assert (o[1][0][keep] - o[0][0][keep]).abs().max().item() <= tol
+
+
+def test_bf16_cache_is_flowkvs(q4):
+    """A bf16 cache that the store has written, read by q4nx_flowkv_decode."""
+    print("[case] bf16 cache and FlowKV", flush=True)
+    rng = np.random.default_rng(22)
+    H, G, d, n, L = 8, 4, 256, 130, 160
+    xh, x = _inputs(rng, n, (H + 2 * G) * d, False)
+    f = torch.from_numpy(_freq(d)).cuda()
+    caches = [torch.full((G, L, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    q = torch.empty(n, H, d, dtype=torch.bfloat16, device="cuda")
+    for a, b in ((0, 129), (129, 130)):
+        q4.q4nx_kv_store(x[a:b, :H * d], x[a:b, H * d:(H + G) * d], x[a:b, (H + G) * d:], _ints(np.arange(a, b)), q[a:b], *caches,
+                         b - a, H, G, d, 1, L, kv_format=q4.Q4NX_KV_BF16, inv_freq=f)
+    o = torch.empty(H, d, device="cuda")
+    q4.q4nx_flowkv_decode(q[n - 1], *caches, H, G, d, L, n - 1, 100, 0.0625, o,
+                          torch.empty(q4.q4nx_flowkv_workspace_size(H, d, L), dtype=torch.uint8, device="cuda"))
+    K, V = (_bits(c[:, :n]) for c in caches)
+    ref, bound, dots = kv4.attention(_bits(q[n - 1:]), K, V, n, 100, 0.0625)
+    tol = (2 * 0.0625 * dots * (d + 4) * U + 2.0 ** -20 + (n + d + 64) * U) * bound
+    assert (np.abs(o.cpu().numpy().astype(np.float64) - ref[0]) <= tol[0]).all()
+    assert torch.isnan(caches[0][:, n:]).all() and torch.isnan(caches[1][:, n:]).all()
+
+
+def test_captured_prompt_and_two_streams(q4):
+    """A call with many rows, captured: replays follow the lengths; two calls at once with a workspace each give what
+    each gives alone."""
+    print("[case] captured prompt, two streams", flush=True)
+    rng = np.random.default_rng(23)
+    H, G, d, L, T, B = 8, 2, 128, 1500, 64, 2
+    caches, _ = _cache(rng, q4, B, G, d, L, [1500, 1500])
+    q = _bf16(oracle.f32_to_bf16(rng.standard_normal((B, T, H, d)).astype(np.float32)))
+    one = q[:, -1:].contiguous()
+    nbytes = [q4.q4nx_kv4_workspace_size(B, t, H, G, d, L) for t in (T, 1)]
+    assert min(nbytes) > 0
+
+    def run(lens, o, work, stream=None):
+        q4.q4nx_kv4_attention(q, *caches, lens, B, T, H, G, d, L, 0, 0.1, o[0], work[0], stream=stream)
+        q4.q4nx_kv4_attention(one, *caches, lens, B, 1, H, G, d, L, 0, 0.1, o[1], work[1], stream=stream)
+
+    def buffers():
+        return ([torch.full((B, t, H, d), float("nan"), device="cuda") for t in (T, 1)],
+                [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in nbytes])
+
+    cases = [[1500, 3], [64, 1500], [0, 700], [1, 513]]
+    want = []
+    for lens in cases:
+        o, work = buffers()
+        run(_ints(lens), o, work)
+        want.append(o)
+    torch.cuda.synchronize()
+    lens, (o, work) = _ints(cases[0]), buffers()
+    stream = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        run(lens, o, work)
+    for case, w in zip(cases + cases, want + want):
+        lens.copy_(_ints(case))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(o, w)), case
+        run(_ints(case), *buffers())                                      # eager work between replays
+
+    streams, sets, at = [torch.cuda.Stream() for _ in range(2)], [buffers() for _ in range(2)], [_ints(c) for c in cases[:2]]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for s, (o, work), lens in zip(streams, sets, at):
+            run(lens, o, work, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for (o, _), w in zip(sets, want) for a, b in zip(o, w))
+
+
+def test_padded_batch(q4):
+    """A step of a batch with a free slot: its token is padding, its length 0; its output is zero, its query untouched."""
+    print("[case] a free slot in a batch", flush=True)
+    rng = np.random.default_rng(24)
+    H, G, d, L, B = 4, 1, 256, 64, 3
+    xh, x = _inputs(rng, B, (H + 2 * G) * d, True)
+    caches, _ = _cache(rng, q4, B, G, d, L, [9, 33, 20], garbage=False)
+    before = [c.clone() for c in caches]
+    q, o = torch.full((B, H, d), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((B, 1, H, d), float("nan"), device="cuda")
+    q4.q4nx_kv_store(x[:, :H * d], x[:, H * d:(H + G) * d], x[:, (H + G) * d:], _ints([9, -1, 20]), q, *caches, B, H, G, d, B, L,
+                     seqs=_ints([0, 1, 2]))
+    q4.q4nx_kv4_attention(q, *caches, _ints([10, 0, 21]), B, 1, H, G, d, L, 0, 0.1, o)
+    assert (q[1] == 7.0).all() and not o[1].any() and torch.isfinite(o).all() and o[0].any() and o[2].any()
+    P = kv4.padded(L)
+    for c, was in zip(caches, before):
+        codes, old = c[:B * G * P * d // 2].view(B, -1), was[:B * G * P * d // 2].view(B, -1)
+        assert torch.equal(codes[1], old[1]) and not torch.equal(codes[0], old[0])
