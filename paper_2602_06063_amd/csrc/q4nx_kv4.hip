@@ -411,7 +411,7 @@ struct AttnArgs {
 static uint32_t reciprocal(int64_t n) { return n == 1 ? 0u : (uint32_t)(((int64_t(1) << 32) + n - 1) / n); }
 __device__ __forceinline__ int over(int x, uint32_t by) { return by ? (int)__umulhi((uint32_t)x, by) : x; }
 
-constexpr int kRowTile = 16, kAttnWaves = 4;
+constexpr int kRowTile = 16, kAttnWaves = 4, kAloneWaves = 8;  // waves of a workgroup among several of a tile, and of one alone
 
 // The running maximum is moved only when a score exceeds it by 2^kSlack: the
 // weights then reach 2^kSlack instead of 1, which rounds no differently, and
@@ -424,6 +424,7 @@ struct TileRange {
   int len, t0, t1, j0, j1;  // positions j0 .. j1 - 1 for rows t0 .. t1
   int blk0, nblk, per;      // blocks, and blocks of a wave
 };
+template <int W>
 __device__ __forceinline__ TileRange tile_range(const AttnArgs& a, int b, int tile) {
   TileRange r;
   r.len = min(max(a.lens[b], 0), a.L);
@@ -433,11 +434,12 @@ __device__ __forceinline__ TileRange tile_range(const AttnArgs& a, int b, int ti
   r.j0 = a.window ? max(0, max(0, r.len - a.T + r.t0) - a.window + 1) : 0;
   r.blk0 = r.j0 / kKvBlock;
   r.nblk = r.j1 > r.j0 ? (r.j1 + kKvBlock - 1) / kKvBlock - r.blk0 : 0;
-  r.per = max(1, over(r.nblk + a.splits * kAttnWaves - 1, a.by_parts));
+  r.per = max(1, over(r.nblk + a.splits * W - 1, a.by_parts));
   return r;
 }
+template <int W>
 __device__ __forceinline__ int active_splits(const TileRange& r) {
-  return r.nblk <= r.per * kAttnWaves ? 1 : (r.nblk + r.per * kAttnWaves - 1) / (r.per * kAttnWaves);
+  return r.nblk <= r.per * W ? 1 : (r.nblk + r.per * W - 1) / (r.per * W);
 }
 
 __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
@@ -473,7 +475,7 @@ __device__ __forceinline__ uint2 v_operand(uint32_t bytes, f32x4 d, f32x4 m) {
 // positions in lane group h are those of V's layout: nothing changes lanes
 // between the two products.
 //
-// grid (splits, row tiles, B G), 4 waves; each wave takes `per` blocks of 32
+// grid (splits, row tiles, B G), W waves; each wave takes `per` blocks of 32
 // positions with a running maximum m and sum l (base 2), and the waves' states
 // are merged through LDS: into the output where the range is one workgroup's,
 // else into the workspace, for kv4_merge_kernel.
@@ -481,19 +483,19 @@ __device__ __forceinline__ uint2 v_operand(uint32_t bytes, f32x4 d, f32x4 m) {
 // The weights exp2(s - m) are rounded to bf16 for the product; NP of them, each
 // the rounding of what the ones before left, keep 8 NP bits: 3 for a float32
 // output, 2 for a bf16 one.
-template <int D, int NP>
-__global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
+template <int D, int NP, int W>
+__global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(AttnArgs a) {
   constexpr int NS = D / 32, NG = D / 32, NT = D / 16;  // K steps, V groups, output tiles
   constexpr int kWords = D / 32;                        // words of K codes per lane and 16 positions
   constexpr int kStride = D + 4;
-  __shared__ __attribute__((aligned(16))) float ys[kAttnWaves][kRowTile][kStride];
-  __shared__ float ms[kAttnWaves][kRowTile], ls[kAttnWaves][kRowTile];
-  __shared__ __attribute__((aligned(16))) float scales[kAttnWaves][D], offsets[kAttnWaves][D];  // V's of a wave's block
+  __shared__ __attribute__((aligned(16))) float ys[W][kRowTile][kStride];
+  __shared__ float ms[W][kRowTile], ls[W][kRowTile];
+  __shared__ __attribute__((aligned(16))) float scales[W][D], offsets[W][D];  // V's of a wave's block
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, h = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int split = blockIdx.x, tile = blockIdx.y, bg = blockIdx.z, b = over(bg, a.by_G), g = bg - b * a.G;
-  const TileRange r = tile_range(a, b, tile);
-  const int active = active_splits(r);
+  const TileRange r = tile_range<W>(a, b, tile);
+  const int active = active_splits<W>(r);
   if (split >= max(active, 1)) return;  // the whole workgroup
 
   const int row = tile * kRowTile + n;
@@ -519,7 +521,7 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
   const uint8_t* vc = a.v + (int64_t)bg * a.P * (D / 2);
   const uint32_t* vp = reinterpret_cast<const uint32_t*>(a.v + a.heads_P * (D / 2)) + (int64_t)bg * a.P * (D / 32);
 
-  const int w0 = r.blk0 + (split * kAttnWaves + wave) * r.per;
+  const int w0 = r.blk0 + (split * W + wave) * r.per;
   const int w1 = min(r.blk0 + r.nblk, w0 + r.per);
 
   uint32_t kw[2][kWords], kpair[2][D == 256 ? 2 : 1];
@@ -688,16 +690,16 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(AttnArgs a) {
   }
   __syncthreads();
   const int nrows = min(kRowTile, a.rows - tile * kRowTile);
-  for (int e = tid; e < nrows * (D / 4); e += 64 * kAttnWaves) {
+  for (int e = tid; e < nrows * (D / 4); e += 64 * W) {
     const int rr = e / (D / 4), dd = 4 * (e - rr * (D / 4));
     float mx = ms[0][rr];
 #pragma unroll
-    for (int w = 1; w < kAttnWaves; ++w) mx = fmaxf(mx, ms[w][rr]);
+    for (int w = 1; w < W; ++w) mx = fmaxf(mx, ms[w][rr]);
     const float base = mx == -INFINITY ? 0.0f : mx;
     float lt = 0.0f;
     f32x4 yt = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float c = __builtin_amdgcn_exp2f(ms[w][rr] - base);
       lt = fmaf(c, ls[w][rr], lt);
       yt += c * *reinterpret_cast<const f32x4*>(&ys[w][rr][dd]);
@@ -765,7 +767,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void kv4_merge_kernel(AttnArgs a,
       const int t0 = over(tile * tile_rows, a.by_hg), t1 = min(a.T - 1, over(tile * tile_rows + tile_rows - 1, a.by_hg));
       active = tile_split(a, block_range(a, len, t0, t1).nblk).active;
     } else {
-      active = active_splits(tile_range(a, b, tile));
+      active = active_splits<kAttnWaves>(tile_range<kAttnWaves>(a, b, tile));
     }
   }
   if (active <= 1) active = 0;
@@ -1223,14 +1225,17 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
 // How a call runs, by the longest range that it allows (lengths are known on
 // the device only).
 //
-// Few rows: kv4_rows_kernel, about two workgroups per CU, none with less than a
-// block of positions for each wave.  Up to kOneGroup values of blocks times d
-// one workgroup takes a tile's whole range and the merge falls away: at d = 256
-// 256 positions take 8.1 us in one launch, 6.0 + 2.7 and the gap in two (8.3
-// and 9.5 us a call, from the host); at d = 128 512 positions 8.3 and 4.8 + 2.9
-// (8.0 and 9.5), at d = 64 1024 positions 9.4 and 4.2 + 3.2 (9.1 and 9.6).
-// Beyond, the two launches win: at d = 256 512 positions are 12.6 and 9.5 us a
-// call.
+// Few rows: kv4_rows_kernel, about two workgroups of 4 waves per CU, none with
+// less than a block of positions for each wave.  Up to kOneGroup (blocks times d),
+// while the CUs hold all tiles at once, a tile's range is one workgroup's of 8
+// waves and the merge falls away.  us of the launches, one and two, without the
+// gap between two of about 1: d = 256 and 256 positions 7.6 and 6.0 + 2.7, 512
+// 11.2 and 6.2 + 2.7; d = 128 and 512 positions 7.4 and 4.8 + 2.9, 1024 11.0
+// and 5.0 + 3.2; d = 64 and 1024 positions 7.7 and 4.2 + 3.2, 2048 12.2 and
+// 4.2 + 3.2; a sequence of 100 positions 4.8 to 6.2 and 5.8 + 1.4.  (One launch
+// of 4 waves: 8.1, 8.4 and 9.4 at the limit.)  More tiles than the CUs hold, a
+// call: d = 256, 400 tiles of 500 positions 17.1 as 8 waves and 15.2 as 4 (150
+// KB of LDS and 75).
 //
 // From tile_rows_from rows of a group on: kv4_expand_kernel and
 // kv4_tiles_kernel, a range split over workgroups where there are fewer tiles
@@ -1251,6 +1256,7 @@ struct AttnPlan {
   int64_t rows, tiles;
   int splits;
   int rw;          // waves of 32 rows in a tile; 0: few rows
+  bool alone;      // few rows: one workgroup of kAloneWaves to a tile
   int64_t cap;     // expanded blocks of a (sequence, group)
   size_t parts_at, bytes;  // of the workspace: where the partials begin, all of it
 };
@@ -1272,7 +1278,8 @@ static AttnPlan attn_plan(int64_t B, int64_t T, int64_t H, int64_t G, int64_t d,
     p.tiles = ceil_div(p.rows, kRowTile);
     const int64_t span = window ? std::min(L, window + std::min<int64_t>(T, kRowTile)) : L;
     const int64_t blocks = ceil_div(span, kKvBlock) + (window ? 1 : 0);
-    if (blocks * d > kOneGroup)
+    p.alone = blocks * d <= kOneGroup && BG * p.tiles * d <= 256 * 256;
+    if (!p.alone)
       p.splits = (int)std::max<int64_t>(1, std::min(kAttnGroups / (BG * p.tiles), ceil_div(blocks, kAttnWaves)));
   }
   p.bytes = p.parts_at + (p.splits == 1 ? 0 : (size_t)(BG * p.tiles * p.splits * tile_rows * (d + 4)) * sizeof(float));
@@ -1299,8 +1306,16 @@ static void launch_attention(const AttnArgs& a, const AttnPlan& p, int64_t BG, b
     else bf16 ? launch_tiles<D, 2, 2, 1>(a, p, BG, stream) : launch_tiles<D, 2, 2, 3>(a, p, BG, stream);
   } else {
     const dim3 grid(p.splits, (unsigned)p.tiles, (unsigned)BG);
-    if (bf16) hipLaunchKernelGGL((kv4_rows_kernel<D, 2>), grid, dim3(64 * kAttnWaves), 0, stream, a);
-    else hipLaunchKernelGGL((kv4_rows_kernel<D, 3>), grid, dim3(64 * kAttnWaves), 0, stream, a);
+    const auto go = [&](auto np, auto w) {
+      hipLaunchKernelGGL((kv4_rows_kernel<D, decltype(np)::value, decltype(w)::value>), grid, dim3(64 * decltype(w)::value), 0,
+                         stream, a);
+    };
+    const auto terms = [&](auto w) {
+      if (bf16) go(std::integral_constant<int, 2>{}, w);
+      else go(std::integral_constant<int, 3>{}, w);
+    };
+    if (p.alone) terms(std::integral_constant<int, kAloneWaves>{});
+    else terms(std::integral_constant<int, kAttnWaves>{});
   }
   if (p.splits == 1) return;
   int slices = 1;
@@ -1508,7 +1523,7 @@ q4nx_status q4nx_kv4_attention(const uint16_t* d_q, const void* d_k, const void*
   a.splits = p.splits;
   a.by_hg = reciprocal(H / G);
   a.by_G = reciprocal(G);
-  a.by_parts = reciprocal(p.rw ? p.splits : (int64_t)p.splits * kAttnWaves);
+  a.by_parts = reciprocal(p.rw ? p.splits : (int64_t)p.splits * (p.alone ? kAloneWaves : kAttnWaves));
   // A scale of zero (equal weights) becomes the smallest normal one, which
   // leaves any finite score below 2^-25 but a masked one at -inf.
   a.scale2 = scale * 1.4426950408889634f;
