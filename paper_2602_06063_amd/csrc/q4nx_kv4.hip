@@ -44,6 +44,14 @@ static inline int64_t kv_positions(int64_t L) { return ceil_div(L, kKvBlock) * k
 // group of 32 values is 8 lanes.  A wave takes 64 / (D / 8) heads of a token
 // at a time, `passes` times, all queries or all keys or all values, so that
 // what they are is the wave's to know and not the lane's.
+//
+// Bound by memory in bytes (every value read once, q written in bf16, k and v in
+// 5 or 16 bits), but of a chunk the vector unit is busy 55 to 70% of the time,
+// most of it with the quantizer's bounds and codes, and the latency of a row's
+// reads, norm and exchanges takes the rest: 4096 tokens of 27B from bf16 41.6 us
+// (111 MB, 2.7 TB/s), 2048 of 4B from float32 13.8 us, one token 4.6 us, which
+// is a launch and two round trips to memory.  Tried without gain: more values
+// requested ahead, fewer registers for more waves.
 struct StoreArgs {
   const void *q, *k, *v;
   const int32_t *positions, *seqs;
@@ -334,7 +342,11 @@ __global__ __launch_bounds__(256) void kv_store_kernel(StoreArgs a) {
 // q4nx_kv4_load
 // ---------------------------------------------------------------------------
 // D / 8 lanes take a row: of K, lane j the word of values 8j..8j+7; of V, the
-// 4 bytes of values 32g + 4i..+3 and + 16 (g = j / 4, i = j % 4).
+// 4 bytes of values 32g + 4i..+3 and + 16 (g = j / 4, i = j % 4).  Rows may come
+// in any order, so each is taken by itself; neighbours, which share the lines
+// of a V block, run on one XCD.  Bound by what it writes and by V's single-byte
+// reads: 32768 rows of 27B's 16 groups 133 us to bf16 (352 MB, 2.6 TB/s), 203 to
+// float32 (620 MB, 3.1 TB/s); one token 2.4 us.
 template <int D, bool F32>
 __device__ __forceinline__ void store4(void* out, int64_t i, f32x4 v) {
   if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + i) = v;
@@ -482,7 +494,13 @@ __device__ __forceinline__ uint2 v_operand(uint32_t bytes, f32x4 d, f32x4 m) {
 //
 // The weights exp2(s - m) are rounded to bf16 for the product; NP of them, each
 // the rounding of what the ones before left, keep 8 NP bits: 3 for a float32
-// output, 2 for a bf16 one.
+// output, 2 for a bf16 one (1 is 5% faster, but then the weights' rounding is as
+// large as the output's, where few rows cost little else).
+//
+// Bound by memory at long ranges: 27B over 32768 positions 21.8 us (84 MB, 3.8
+// TB/s, a copy reaches 4.8), over 131072 80 us (4.2 TB/s); the vector unit, which
+// turns codes into bf16, is busy 70% of that.  Short ranges are bound by latency:
+// a launch, the length, a block's two products, 4.2 to 6.2 us.
 template <int D, int NP, int W>
 __global__ __launch_bounds__(64 * W, 2) void kv4_rows_kernel(AttnArgs a) {
   constexpr int NS = D / 32, NG = D / 32, NT = D / 16;  // K steps, V groups, output tiles
@@ -731,14 +749,18 @@ __device__ __forceinline__ BlockRange block_range(const AttnArgs& a, int len, in
 }
 
 // How a workgroup of kv4_tiles_kernel shares the blocks of its tile: splits of
-// at least kTileBlocks blocks, an even number.
-constexpr int kTileBlocks = 16;
+// at least tile_blocks blocks, an even number.  us with 8, 16 and 32: d = 128,
+// 16 groups, 400 rows over 2048 positions (4 splits of 16) 15.5, 13.4 and 17.3;
+// d = 256, one workgroup to a CU, 4 groups, 256 rows over 2048 17.6, 20.8 and
+// 29.5, one group, 1024 rows over 1024 16.2, 20.4 and 28.9.
+constexpr int tile_blocks(int64_t d) { return d == 256 ? 8 : 16; }
 struct TileSplit {
   int per, active;
 };
+template <int D>
 __device__ __forceinline__ TileSplit tile_split(const AttnArgs& a, int nblk) {
   TileSplit s;
-  s.per = max(kTileBlocks, (over(nblk + a.splits - 1, a.by_parts) + 1) & ~1);
+  s.per = max(tile_blocks(D), (over(nblk + a.splits - 1, a.by_parts) + 1) & ~1);
   s.active = nblk <= s.per ? 1 : (nblk + s.per - 1) / s.per;
   return s;
 }
@@ -747,7 +769,8 @@ __device__ __forceinline__ TileSplit tile_split(const AttnArgs& a, int nblk) {
 // launch has written): partials [B G][tile][split][row of the tile][m, l, -, -,
 // D values].  A wave takes 64 values of a row, or 1 / `slices` of the splits of
 // them (slices waves, a power of two, then merge through LDS in order): every
-// slices-th split, eight at a time (one round trip to memory).
+// slices-th split, eight at a time (one round trip to memory).  Bound by
+// latency: 1.4 us where nothing is to be merged, 2.7 for two splits, 4.6 for 32.
 // grid (8 / slices units of 64 values each, B G).
 constexpr int kMergeAhead = 8, kMergeWaves = 8;
 template <int D, bool TILES>
@@ -765,7 +788,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void kv4_merge_kernel(AttnArgs a,
     if constexpr (TILES) {
       const int len = min(max(a.lens[b], 0), a.L);
       const int t0 = over(tile * tile_rows, a.by_hg), t1 = min(a.T - 1, over(tile * tile_rows + tile_rows - 1, a.by_hg));
-      active = tile_split(a, block_range(a, len, t0, t1).nblk).active;
+      active = tile_split<D>(a, block_range(a, len, t0, t1).nblk).active;
     } else {
       active = active_splits<kAttnWaves>(tile_range<kAttnWaves>(a, b, tile));
     }
@@ -838,7 +861,9 @@ __global__ __launch_bounds__(64 * kMergeWaves) void kv4_merge_kernel(AttnArgs a,
 //      16s + 8 (e / 4) + 4h + e % 4, where the score product of 32 positions
 //      leaves the weights of lane half h
 // Positions that no row attends to are zeros.  grid (blocks, B G, K and V).
-constexpr int kExpandGroups = 2048;
+// Bound by its writes: 8192 positions of 27B's 16 groups 25 us (88 MB, 3.5 TB/s),
+// 6% of what a chunk of 4096 tokens then takes with them.
+constexpr int kExpandGroups = 4096;  // (of 32768 positions of 4B, 50 us, with 2048 54 and 1024 58)
 
 // The first block that any row of the sequence attends to.
 __device__ __forceinline__ int first_block(const AttnArgs& a, int len) {
@@ -944,9 +969,19 @@ __device__ __forceinline__ void copy_one(const u32x4* src, const uint32_t (&offs
 // takes the exponentials of this one, so that the matrix unit works under the
 // vector unit's share of the step: K is a step ahead of V.
 //
-// grid (tiles, splits): tiles with the longest ranges first, neighbours of one another on
-// different groups, so that each XCD (workgroups are dealt out to the 8 in
-// turn) works on few groups at a time.
+// The weights are one bf16 term for a bf16 output (their rounding, half a step of
+// the output's type at most, averages out over the positions) and three for a
+// float32 one, which doubles the matrix work.  Bound by the matrix unit and the
+// clock that the card holds under it (1.75 to 1.9 GHz): 4096 tokens of 27B over
+// 8192 positions 428 us, 0.97 PFLOP/s of the 1.2 that a large matrix product
+// reaches here; 777 tokens of a window of 1024, float32, 40 us; 4B's first 2048
+// tokens 53 us, the longest tile's 32 steps of 1.2 us and its beginning and end
+// (a tile to a CU, half of the CUs' time idle on average).
+//
+// grid (tiles, splits): tiles with the longest ranges first, neighbours of one
+// another on different groups, so that each XCD (workgroups are dealt out to the
+// 8 in turn) works on few groups at a time.
+
 // Orders what stands between scheduling barriers: N times a matrix
 // instruction, V vector ones that run under it, a read of LDS and a copy into it
 // (copies in a row hold their wave up, 16 clocks each).
@@ -988,7 +1023,7 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
   // rows see.
   const int base = __builtin_amdgcn_readfirstlane(first_block(a, len));
   const BlockRange all = block_range(a, len, over(tile * kRows, a.by_hg), min(a.T - 1, over(tile * kRows + kRows - 1, a.by_hg)));
-  const TileSplit split = tile_split(a, all.nblk);
+  const TileSplit split = tile_split<D>(a, all.nblk);
   const int at = blockIdx.y * split.per;
   if (blockIdx.y > 0 && at >= all.nblk) return;  // the whole workgroup
   const int blk0 = __builtin_amdgcn_readfirstlane(all.blk0 + at);
@@ -1272,7 +1307,7 @@ static AttnPlan attn_plan(int64_t B, int64_t T, int64_t H, int64_t G, int64_t d,
     p.rw = BG * ceil_div(p.rows, 128) >= 512 ? 4 : 2;
     tile_rows = 32 * p.rw;
     p.tiles = ceil_div(p.rows, tile_rows);
-    p.splits = (int)std::max<int64_t>(1, std::min((d == 256 ? 256 : 512) / (BG * p.tiles), ceil_div(p.cap, kTileBlocks)));
+    p.splits = (int)std::max<int64_t>(1, std::min((d == 256 ? 256 : 512) / (BG * p.tiles), ceil_div(p.cap, tile_blocks(d))));
     p.parts_at = (size_t)(BG * p.cap + 1) * (size_t)(2 * kKvBlock * d * 2);  // (a step may copy a block past the last)
   } else {
     p.tiles = ceil_div(p.rows, kRowTile);
@@ -1331,6 +1366,8 @@ static void launch_attention(const AttnArgs& a, const AttnPlan& p, int64_t BG, b
 }
 
 // ---- launchers ------------------------------------------------------------
+// Waves that a chunk is cut into (4096, 8192 and 16384: 2048 tokens of 4B 13.2,
+// 13.2 and 14.9 us, 4096 of 27B 42.1, 42.2 and 41.4).
 constexpr int64_t kStoreWaves = 8192;
 template <int D, bool F32, bool Q4>
 static void launch_store(const StoreArgs& a, hipStream_t stream) {
