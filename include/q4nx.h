@@ -394,16 +394,16 @@ size_t q4nx_kv4_workspace_size(int64_t B, int64_t T, int64_t H, int64_t G, int64
  *   d_o    : device, [B][T][H][d] of o_dtype; fully written
  *   d_work : device, at least q4nx_kv4_workspace_size bytes, owned by the
  *            caller (NULL where that is 0); contents on entry do not matter.
- *            Calls that share a workspace must not overlap.  With few rows
- *            it holds partial results (some MB); with many (T H/G from 192 on,
- *            from 256 at d = 256) also K and V of the attended range in bf16,
- *            4 d bytes a position of each sequence and group.
+ *            Calls that share a workspace must not overlap.  It holds partial
+ *            results (some MB), and for many rows over a long range (a prompt's
+ *            chunk from some hundred tokens on) also K and V of the attended
+ *            range in bf16, 4 d bytes a position of each sequence and group.
  * Pointers are 16-byte aligned where nothing else is said.  Scores are float32
  * sums of exact bf16 products, exponentials and sums float32.  A weight of a
  * value enters the product as a sum of bf16 terms: three for a float32 output,
- * which keeps float32 accuracy; for a bf16 output two with few rows (2^-16 of
- * the weight), and one with many (2^-8 at most, as the output's own rounding,
- * and of either sign from position to position).  The order of the sums depends on B, T, H, G, d, L, window and the
+ * which keeps float32 accuracy; for a bf16 output two (2^-16 of the weight), or
+ * one for many rows over a long range (2^-8 at most, as the output's own
+ * rounding, and of either sign from position to position).  The order of the sums depends on B, T, H, G, d, L, window and the
  * lengths alone: the same call gives the same bits every time.
  * Errors: Q4NX_ERR_INVALID_ARG (NULL pointer, unknown dtype, non-finite
  * scale), Q4NX_ERR_SHAPE, Q4NX_ERR_ALIGNMENT, Q4NX_ERR_BUFFER_TOO_SMALL,

@@ -1272,13 +1272,21 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
 // call: d = 256, 400 tiles of 500 positions 17.1 as 8 waves and 15.2 as 4 (150
 // KB of LDS and 75).
 //
-// From tile_rows_from rows of a group on: kv4_expand_kernel and
-// kv4_tiles_kernel, a range split over workgroups where there are fewer tiles
-// than they can be.  Measured, all launches of each side: d = 256, 4 groups, 128
-// rows over 4096 positions 25 us as few rows and 35 as tiles, over 32768 83 and
-// 109; 256 rows 37 and 36, 151 and 122.  d = 128, 16 groups, 128 rows 29 and
-// 32, 162 and 160; 256 rows 50 and 40, 317 and 195.  d = 64, 16 groups, 128
-// rows 20 and 23, 97 and 88.
+// Many rows over long ranges, 192 of a group on and more tiles of 16 rows times
+// blocks than few_tiles: kv4_expand_kernel and kv4_tiles_kernel, a range split
+// over workgroups where there are fewer tiles than they can be.  us of all
+// launches, few rows and tiles, by tiles x blocks in thousands:
+//   d = 256: 1B 1024 rows (256 tokens) alone 0.5: 10 and 20; 4B 1024 rows over
+//     1024 positions 8: 36 and 37; 384 over 4096 12: 41 and 43; 512 over 4096 16:
+//     47 and 42; 192 over 16384 25: 64 and 72; 256 over 16384 33: 76 and 74; 2048
+//     over 4096 65: 131 and 86; 1B 512 over 16384 16: 46 and 47, 2048 over 4096
+//     16: 48 and 40
+//   d = 128, 16 groups: 256 over 1024 8: 21 and 27; 512 over 1024 16: 22 and 32;
+//     1024 over 512 16: 22 and 18; 256 over 4096 33: 45 and 42; 1024 over 1024
+//     33: 37 and 46; 384 over 4096 49: 67 and 46; 1024 over 4096 131: 126 and 77;
+//     128 over 16384 65: 77 and 94
+//   d = 64, 16 groups: 1024 over 1024 33: 23 and 30; 256 over 4096 33: 29 and 28;
+//     384 over 4096 49: 43 and 32; 128 over 16384 65: 49 and 51
 //
 // Tiles of 128 rows (every operand read by 4 waves) from 512 of them on, else of
 // 64 with two key parts: d = 128, 16 groups, a prompt of 2048 tokens (512 tiles)
@@ -1286,7 +1294,8 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
 // d = 256, 4 groups, 2048 tokens (128 tiles) 90 and 52.
 constexpr int kAttnGroups = 512;
 constexpr int64_t kOneGroup = 2048;
-static int64_t tile_rows_from(int64_t d) { return d == 256 ? 256 : 192; }
+constexpr int64_t kManyRows = 192;
+static int64_t few_tiles(int64_t d) { return d == 256 ? 16383 : 32768; }
 struct AttnPlan {
   int64_t rows, tiles;
   int splits;
@@ -1301,18 +1310,18 @@ static AttnPlan attn_plan(int64_t B, int64_t T, int64_t H, int64_t G, int64_t d,
   const int64_t BG = B * G;
   p.rows = T * (H / G);
   int64_t tile_rows = kRowTile;
-  if (p.rows >= tile_rows_from(d)) {
-    const int64_t span = window ? std::min(L, window - 1 + T) : L;
-    p.cap = std::min(ceil_div(span, kKvBlock) + 1, kv_positions(L) / kKvBlock);
+  p.tiles = ceil_div(p.rows, kRowTile);
+  const int64_t span = window ? std::min(L, window + std::min<int64_t>(T, kRowTile)) : L;
+  const int64_t blocks = ceil_div(span, kKvBlock) + (window ? 1 : 0);
+  if (p.rows >= kManyRows && BG * p.tiles * blocks > few_tiles(d)) {
+    const int64_t all = window ? std::min(L, window - 1 + T) : L;
+    p.cap = std::min(ceil_div(all, kKvBlock) + 1, kv_positions(L) / kKvBlock);
     p.rw = BG * ceil_div(p.rows, 128) >= 512 ? 4 : 2;
     tile_rows = 32 * p.rw;
     p.tiles = ceil_div(p.rows, tile_rows);
     p.splits = (int)std::max<int64_t>(1, std::min((d == 256 ? 256 : 512) / (BG * p.tiles), ceil_div(p.cap, tile_blocks(d))));
     p.parts_at = (size_t)(BG * p.cap + 1) * (size_t)(2 * kKvBlock * d * 2);  // (a step may copy a block past the last)
   } else {
-    p.tiles = ceil_div(p.rows, kRowTile);
-    const int64_t span = window ? std::min(L, window + std::min<int64_t>(T, kRowTile)) : L;
-    const int64_t blocks = ceil_div(span, kKvBlock) + (window ? 1 : 0);
     p.alone = blocks * d <= kOneGroup && BG * p.tiles * d <= 256 * 256;
     if (!p.alone)
       p.splits = (int)std::max<int64_t>(1, std::min(kAttnGroups / (BG * p.tiles), ceil_div(blocks, kAttnWaves)));

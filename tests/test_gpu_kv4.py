@@ -9,8 +9,8 @@ Tolerances (derived, none fitted):
   values, and keys that are neither normed nor rotated: the bytes themselves.
   attention with u = 2^-24: a score is off by at most d u sum|q k| scale + 4 u |s|, so a weight by e = 2 x that (itself and
             the sum) + 2^-20 (exponentials, corrections); the sums over n positions add (n + 64) u; the weights' rounding
-            2^-24 for a float32 output; for a bf16 one 2^-16 with few rows (two bf16 terms) and 2^-8 with many (one term:
-            half a step of bf16, as the output's own rounding): e' sum p|v|.  Then the output's rounding.
+            2^-24 for a float32 output; for a bf16 one 2^-16 (two bf16 terms), or 2^-8 with many rows over a long range
+            (one term: half a step of bf16, as the output's own rounding): e' sum p|v|.  Then the output's rounding.
 """
 import numpy as np
 import pytest
@@ -270,6 +270,18 @@ def _cache(rng, q4, B, G, d, L, lens, garbage=True):
     return out, values
 
 
+def _tiled(B, T, H, G, d, L, window):
+    """Whether a call expands K and V and works in tiles of many rows."""
+    rows, span = T * H // G, min(L, window + min(T, 16)) if window else L
+    blocks = -(-span // 32) + (window > 0)
+    return rows >= 192 and B * G * -(-rows // 16) * blocks > (16383 if d == 256 else 32768)
+
+
+def _long(B, T, H, G, d):
+    """A capacity from which on such a call does."""
+    return 32 * (33000 // (B * G * -(-T * H // G // 16)) + 1)
+
+
 def _check_attention(q4, H, G, d, lens, T, window, bf16, L=None, scale=None, seed=0, spread=1.5):
     print("[case] attention", H, G, d, lens, T, window, bf16, L, flush=True)
     rng = np.random.default_rng(seed + H + T)
@@ -291,7 +303,7 @@ def _check_attention(q4, H, G, d, lens, T, window, bf16, L=None, scale=None, see
     for b in range(B):
         ref, bound, dots = kv4.attention(q[b], K[b], V[b], lens[b], window, scale)
         ds = abs(scale) * dots * (d * U + 4 * U)
-        rounding = 2.0 ** -24 if not bf16 else 2.0 ** -16 if T * H // G < (256 if d == 256 else 192) else 2.0 ** -8
+        rounding = 2.0 ** -24 if not bf16 else 2.0 ** -8 if _tiled(B, T, H, G, d, L, window) else 2.0 ** -16
         e = 2 * ds + 2.0 ** -20 + (lens[b] + 64) * U + rounding
         tol = e * bound + (2.0 ** -8 if bf16 else U) * np.abs(ref) + 1e-37
         err = np.abs(got[b] - ref)
@@ -329,7 +341,7 @@ def _check_attention(q4, H, G, d, lens, T, window, bf16, L=None, scale=None, see
     (3, 1, 128, [300], 130, 17, False, 512),
     (16, 16, 64, [120], 120, 0, True, 120),
     (16, 1, 64, [90], 90, 40, False, 90),
-    # many rows (192 of a group on, 256 at d = 256): tiles of 64 rows (two key parts) and, from 512 of 128 on, of 128; a
+    # many rows over short ranges, and in test_attention_tiles over long ones: tiles of 64 rows (two key parts) and, from 512 of 128 on, of 128; a
     # tile's last rows missing; a sequence shorter than its rows, and an empty one; windows that leave whole blocks of a
     # tile to some rows only
     (8, 4, 128, [333], 100, 0, False, 400),
@@ -345,7 +357,7 @@ def _check_attention(q4, H, G, d, lens, T, window, bf16, L=None, scale=None, see
     (64, 64, 128, [250, 192, 5, 0], 192, 50, False, 260),
     (64, 64, 256, [300, 256, 5, 0], 256, 0, False, 300),
     (64, 64, 256, [300, 256, 5, 0], 256, 33, True, 300),
-    # tiles whose range is split: whole and ragged last splits, a sequence with one split beside one with several
+    # whole and ragged last splits, a sequence with one split beside one with several
     (4, 2, 128, [2100, 513, 40], 100, 0, False, 2200),
     (8, 1, 64, [1600], 27, 0, True, 4000),
     (4, 2, 256, [1057], 129, 0, False, 1057),
@@ -355,6 +367,42 @@ def _check_attention(q4, H, G, d, lens, T, window, bf16, L=None, scale=None, see
 ])
 def test_attention(q4, H, G, d, lens, T, window, bf16, L):
     _check_attention(q4, H, G, d, lens, T, window, bf16, L)
+
+
+# Many rows over long ranges (L None: a capacity that makes it one, however short the sequences): the cases of many rows
+# above, tiles whose range is split and not, windows inside a tile's range and across splits, on tiles of 64 rows and 128.
+@pytest.mark.parametrize("H,G,d,lens,T,window,bf16,L", [
+    (8, 4, 128, [333], 100, 0, False, None),
+    (8, 4, 256, [333], 333, 0, True, None),
+    (12, 4, 64, [700, 40, 0], 64, 0, False, None),
+    (16, 16, 64, [220], 220, 0, True, None),
+    (6, 2, 256, [2100], 90, 0, True, None),
+    (64, 64, 64, [250, 192, 5, 0], 192, 0, False, 1000),
+    (64, 64, 64, [250, 192, 5, 0], 192, 0, True, 1000),
+    (64, 64, 128, [250, 192, 5, 0], 192, 0, False, 1000),
+    (64, 64, 256, [300, 256, 5, 0], 256, 0, False, 300),
+    (4, 2, 128, [2100, 513, 40], 100, 0, False, None),
+    (8, 1, 64, [1600], 27, 0, True, None),
+    (4, 2, 256, [1057], 129, 0, False, None),
+    (32, 32, 128, [2000], 512, 1100, False, 2100),
+    (32, 32, 64, [2000], 512, 1100, True, 2100),
+    (100, 100, 64, [700], 512, 300, False, 800),
+    (512, 512, 64, [300], 272, 50, False, 300),
+    (700, 700, 64, [300], 272, 33, True, 300),
+    (64, 64, 256, [700], 520, 200, True, 700),
+    (20, 20, 128, [1500], 1500, 0, False, 1500),
+])
+def test_attention_tiles(q4, H, G, d, lens, T, window, bf16, L):
+    L = L or max(_long(len(lens), T, H, G, d), max(lens))
+    assert _tiled(len(lens), T, H, G, d, L, window)
+    _check_attention(q4, H, G, d, lens, T, window, bf16, L)
+
+
+def test_attention_tiles_peaked_and_flat(q4):
+    L = _long(1, 110, 4, 2, 128)
+    _check_attention(q4, 4, 2, 128, [400], 110, 0, False, L, scale=-0.3)
+    _check_attention(q4, 4, 2, 128, [400], 110, 0, False, L, scale=1e-30)
+    _check_attention(q4, 4, 2, 128, [400], 110, 0, False, L, spread=20.0)
 
 
 def test_attention_peaked_and_flat(q4):
@@ -535,16 +583,18 @@ def test_a_nan_query_stays_in_its_row(q4):
     print("[case] NaN query rows", flush=True)
     rng = np.random.default_rng(21)
     H, G, d, n = 8, 2, 128, 700
-    caches, _ = _cache(rng, q4, 1, G, d, n, [n])
+    L = _long(1, 60, H, G, d)
+    assert _tiled(1, 60, H, G, d, L, 0)
+    caches, _ = _cache(rng, q4, 1, G, d, L, [n])
     for T in (1, 5, 60):                                                  # one tile, two, and tiles of 64 rows
         q = _bf16(oracle.f32_to_bf16(rng.standard_normal((1, T, H, d)).astype(np.float32)))
         bad = q.clone()
         bad[0, T // 2, 1] = float("nan")
         bad[0, 0, 6, 3] = float("inf")
-        work = torch.empty(max(16, q4.q4nx_kv4_workspace_size(1, T, H, G, d, n)), dtype=torch.uint8, device="cuda")
+        work = torch.empty(max(16, q4.q4nx_kv4_workspace_size(1, T, H, G, d, L)), dtype=torch.uint8, device="cuda")
         o = [torch.empty(1, T, H, d, device="cuda") for _ in range(2)]
         for x, y in zip((q, bad), o):
-            q4.q4nx_kv4_attention(x, *caches, _ints([n]), 1, T, H, G, d, n, 0, 0.1, y, work)
+            q4.q4nx_kv4_attention(x, *caches, _ints([n]), 1, T, H, G, d, L, 0, 0.1, y, work)
         assert torch.isnan(o[1][0, T // 2, 1]).all() and torch.isnan(o[1][0, 0, 6]).all() and torch.isfinite(o[0]).all()
         keep = torch.ones(T, H, dtype=torch.bool, device="cuda")
         keep[T // 2, 1] = keep[0, 6] = False
@@ -580,7 +630,8 @@ def test_captured_prompt_and_two_streams(q4):
     each gives alone."""
     print("[case] captured prompt, two streams", flush=True)
     rng = np.random.default_rng(23)
-    H, G, d, L, T, B = 8, 2, 128, 1500, 64, 2
+    H, G, d, L, T, B = 8, 2, 128, 17000, 64, 2
+    assert _tiled(B, T, H, G, d, L, 0)
     caches, _ = _cache(rng, q4, B, G, d, L, [1500, 1500])
     q = _bf16(oracle.f32_to_bf16(rng.standard_normal((B, T, H, d)).astype(np.float32)))
     one = q[:, -1:].contiguous()
