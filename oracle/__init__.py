@@ -1,5 +1,6 @@
 """CPU oracle for the Q4NX projection path and its next steps (the quantizer
-into Q4NX, FlowKV decode attention, the MXFP4 block variant) -- TEST
+into Q4NX, FlowKV decode attention, the MXFP4 block variant, the 4-bit KV
+cache) -- TEST
 INFRASTRUCTURE ONLY.
 
 A plain, slow, obviously correct NumPy implementation of what the GPU path
