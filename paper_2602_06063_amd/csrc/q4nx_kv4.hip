@@ -1278,15 +1278,18 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
 // launches, few rows and tiles, by tiles x blocks in thousands:
 //   d = 256: 1B 1024 rows (256 tokens) alone 0.5: 10 and 20; 4B 1024 rows over
 //     1024 positions 8: 36 and 37; 384 over 4096 12: 41 and 43; 512 over 4096 16:
-//     47 and 42; 192 over 16384 25: 64 and 72; 256 over 16384 33: 76 and 74; 2048
-//     over 4096 65: 131 and 86; 1B 512 over 16384 16: 46 and 47, 2048 over 4096
-//     16: 48 and 40
+//     47 and 42; 8 sequences of 256 over 1024 16: 29 and 51; 2048 in a window of
+//     1024 17: 44 and 56; 192 over 16384 25: 64 and 72; 768 over 4096 25: 77 and
+//     50; 256 over 16384 33: 76 and 74; 2048 over 4096 65: 131 and 86; 1B 512
+//     over 16384 16: 46 and 47, 2048 over 4096 16: 48 and 40
 //   d = 128, 16 groups: 256 over 1024 8: 21 and 27; 512 over 1024 16: 22 and 32;
 //     1024 over 512 16: 22 and 18; 256 over 4096 33: 45 and 42; 1024 over 1024
 //     33: 37 and 46; 384 over 4096 49: 67 and 46; 1024 over 4096 131: 126 and 77;
 //     128 over 16384 65: 77 and 94
 //   d = 64, 16 groups: 1024 over 1024 33: 23 and 30; 256 over 4096 33: 29 and 28;
 //     384 over 4096 49: 43 and 32; 128 over 16384 65: 49 and 51
+// (bf16 outputs; with float32 ones, whose tiles take longer, the two meet at the
+// same places: d = 128, 256 over 4096 48 and 49, 512 over 4096 77 and 65.)
 //
 // Tiles of 128 rows (every operand read by 4 waves) from 512 of them on, else of
 // 64 with two key parts: d = 128, 16 groups, a prompt of 2048 tokens (512 tiles)
@@ -1295,7 +1298,7 @@ __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void kv4_tiles_kern
 constexpr int kAttnGroups = 512;
 constexpr int64_t kOneGroup = 2048;
 constexpr int64_t kManyRows = 192;
-static int64_t few_tiles(int64_t d) { return d == 256 ? 16383 : 32768; }
+static int64_t few_tiles(int64_t d) { return d == 256 ? 20480 : 32768; }
 struct AttnPlan {
   int64_t rows, tiles;
   int splits;

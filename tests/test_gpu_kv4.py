@@ -274,7 +274,7 @@ def _tiled(B, T, H, G, d, L, window):
     """Whether a call expands K and V and works in tiles of many rows."""
     rows, span = T * H // G, min(L, window + min(T, 16)) if window else L
     blocks = -(-span // 32) + (window > 0)
-    return rows >= 192 and B * G * -(-rows // 16) * blocks > (16383 if d == 256 else 32768)
+    return rows >= 192 and B * G * -(-rows // 16) * blocks > (20480 if d == 256 else 32768)
 
 
 def _long(B, T, H, G, d):
@@ -389,7 +389,7 @@ def test_attention(q4, H, G, d, lens, T, window, bf16, L):
     (100, 100, 64, [700], 512, 300, False, 800),
     (512, 512, 64, [300], 272, 50, False, 300),
     (700, 700, 64, [300], 272, 33, True, 300),
-    (64, 64, 256, [700], 520, 200, True, 700),
+    (64, 64, 256, [700], 520, 280, True, 700),
     (20, 20, 128, [1500], 1500, 0, False, 1500),
 ])
 def test_attention_tiles(q4, H, G, d, lens, T, window, bf16, L):
